@@ -394,6 +394,60 @@ mllm_status_t mllm_op_colsum_static(const void* x, float* out, int accumulate, i
                                     void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * The token side of a language model: what a training step does in front of the first decoder stage and behind the last
+ * one (the head's products are mllm_op_gemm and mllm_op_linear_bwd), and the per-head QK normalisation of a decoder or encoder
+ * layer.  Row strides are in elements and multiples of 8; bf16 and fp32 matrices start on 16 bytes (MLLM_ERR_UNSUPPORTED
+ * otherwise).  None of these calls copies from the host, so all may be captured into a graph.  Sums are fp32 and each bf16 result is rounded once.
+ * ------------------------------------------------------------------------------------------ */
+
+/* Token rows of the packed sequence: y [t, d] bf16 = scale * table[ids[i]], table [vocab, d] bf16 (table_fp32 0) or fp32 (1), ids device
+ * int32 [t], rows of y y_stride apart, d a multiple of 8.  A row whose id is negative names no token (the rows of image tokens, which
+ * the connector fills) and becomes zero; an id at or beyond vocab reads nothing and makes its row NaN.  y must not overlap the table. */
+mllm_status_t mllm_op_embed_fwd(const void* table, int table_fp32, const int32_t* ids, void* y, int64_t t, int64_t vocab,
+                                int64_t d, int64_t y_stride, float scale, void* hip_stream);
+/* The table's gradient: dtable [vocab, d] fp32 = scale * (sum of the rows of dy whose id it is, in the order of the tokens);
+ * accumulate != 0: added to what dtable holds, rows of other ids untouched.  dy bf16 [t, d], rows dy_stride apart.  Ids outside
+ * [0, vocab) contribute nothing.  workspace: mllm_op_embed_bwd_workspace_bytes, 256-byte aligned, contents undefined afterwards (the
+ * token lists by id and partial sums; the same bytes serve fewer tokens with the same vocab and d). */
+size_t mllm_op_embed_bwd_workspace_bytes(int64_t t, int64_t vocab, int64_t d);
+mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab,
+                                int64_t d, int64_t dy_stride, float scale, void* workspace, size_t workspace_bytes,
+                                void* hip_stream);
+
+/* Per-head QK normalisation with the rotary positions in the same pass.  x bf16 [t, x_stride]: the leading n_q_heads + n_kv_heads heads
+ * of head_dim columns of every row are the query and key heads (as in a packed [q | k | v] row).  Each head is replaced by
+ * n = head * rsqrt(mean(head^2) + eps) * gamma (gamma_q or gamma_k, bf16 [head_dim], shared by the heads) and, with a
+ * rope_table (device fp32 [n_pos, head_dim] from mllm_op_rope_table), rotated in half-split pairs by the angle of pos[row] (device
+ * int32 [t]); without one (rope_table NULL, pos and n_pos ignored) it is only normalised.  A position outside [0, n_pos) reads
+ * nothing and makes the row's heads NaN.  y receives the same columns (rows y_stride apart), other columns are not touched; y may be
+ * x with the same stride.  head_dim: a multiple of 16, at most 256. */
+mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const void* gamma_k, void* y, const int32_t* pos,
+                                       const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int64_t x_stride, int64_t y_stride, float eps, void* hip_stream);
+/* Its gradients, from dy (the gradient of y) and the x that entered: dx in the same columns (rows dx_stride apart; dx may be dy or
+ * x with the same stride), dgamma_q and dgamma_k fp32 [head_dim] (accumulate != 0: +=).  With the gradient of the
+ * rotation already taken (mllm_op_attn_bwd_rope) pass no rope_table.  partial: fp32 scratch of
+ * mllm_op_qk_norm_rope_bwd_partial_bytes. */
+size_t mllm_op_qk_norm_rope_bwd_partial_bytes(int64_t t, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim);
+mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void* gamma_q, const void* gamma_k, void* dx,
+                                       float* dgamma_q, float* dgamma_k, int accumulate, float* partial, const int32_t* pos,
+                                       const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int64_t dy_stride, int64_t x_stride, int64_t dx_stride, float eps,
+                                       void* hip_stream);
+
+/* Softmax cross-entropy of every row and the gradient of its logits, in one call.  logits [t, cols], bf16 (logits_fp32 0) or fp32 (1),
+ * rows logits_stride apart, cols a multiple of 8; the first vocab (<= cols) columns are the vocabulary, what lies behind them is
+ * never used.  targets device int32 [t]:
+ *   loss [t] fp32 = log(sum over j < vocab of exp(logits[i][j])) - logits[i][targets[i]], 0 where the target is negative
+ *   dlogits [t, cols] bf16 = scale * dloss[i] * (softmax(logits[i]) - onehot(targets[i])), rows with a negative target and columns from
+ *   vocab on 0; rows dlogits_stride apart; NULL: the loss alone.  dloss fp32 [t], the weight of every row's loss; NULL: 1.
+ * dlogits may be logits (bf16, same stride).  The logits of a row with a negative target are not read.  Logits of -inf have probability 0
+ * (a target among them: loss +inf); a row that is all -inf, holds +inf or NaN, or whose target is at or beyond vocab gives NaN. */
+mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* targets, const float* dloss, float* loss,
+                           void* dlogits, int64_t t, int32_t vocab, int32_t cols, int64_t logits_stride, int64_t dlogits_stride,
+                           float scale, void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Online microbatch scheduler (host only, no GPU work; Online Microbatch Scheduler, "Problem
  * Formulation" and "Scheduling Optimization").  Item i of a global batch has an encoder-stage
  * duration e_dur[i] and an LLM-stage duration l_dur[i] (host arrays, non-negative).  The items are

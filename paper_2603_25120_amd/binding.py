@@ -24,7 +24,9 @@ EXPORTS = ["mllm_stage_create", "mllm_stage_destroy", "mllm_stage_param_count", 
            "mllm_stage_sizes", "mllm_stage_fwd", "mllm_stage_bwd", "mllm_last_error", "mllm_op_gemm",
            "mllm_gemm_form", "mllm_op_linear_bwd", "mllm_linear_bwd_form", "mllm_op_gemm_swiglu", "mllm_op_gemm_swiglu_bwd", "mllm_op_attn_workspace_bytes", "mllm_attn_work_list", "mllm_op_attn_fwd", "mllm_op_attn_bwd", "mllm_op_norm_fwd",
            "mllm_op_norm_bwd_partial_bytes", "mllm_op_norm_bwd", "mllm_op_norm_bwd_colsum", "mllm_op_rope", "mllm_op_rope_table", "mllm_op_gemm_rope", "mllm_op_attn_bwd_rope", "mllm_op_act_fwd",
-           "mllm_op_act_bwd", "mllm_op_colsum_partial_bytes", "mllm_op_colsum", "mllm_op_colsum_static_max_bytes", "mllm_op_colsum_static", "mllm_profile_begin",
+           "mllm_op_act_bwd", "mllm_op_colsum_partial_bytes", "mllm_op_colsum", "mllm_op_colsum_static_max_bytes", "mllm_op_colsum_static",
+           "mllm_op_embed_fwd", "mllm_op_embed_bwd_workspace_bytes", "mllm_op_embed_bwd", "mllm_op_qk_norm_rope_fwd",
+           "mllm_op_qk_norm_rope_bwd_partial_bytes", "mllm_op_qk_norm_rope_bwd", "mllm_op_xent", "mllm_profile_begin",
            "mllm_profile_end", "mllm_schedule_lpt", "mllm_schedule", "mllm_interp", "mllm_item_durations",
            "mllm_find_combs", "mllm_evaluate_parallelism", "mllm_optimize_parallelism"]
 
@@ -135,6 +137,15 @@ def lib() -> C.CDLL:
     L.mllm_op_colsum_static_max_bytes.argtypes = []
     L.mllm_op_colsum_static_max_bytes.restype = sz
     L.mllm_op_colsum_static.argtypes = [vp, vp, C.c_int, i64, i64, vp]
+    L.mllm_op_embed_fwd.argtypes = [vp, C.c_int, vp, vp, i64, i64, i64, i64, C.c_float, vp]
+    L.mllm_op_embed_bwd_workspace_bytes.argtypes = [i64, i64, i64]
+    L.mllm_op_embed_bwd_workspace_bytes.restype = sz
+    L.mllm_op_embed_bwd.argtypes = [vp, vp, vp, C.c_int, i64, i64, i64, i64, C.c_float, vp, sz, vp]
+    L.mllm_op_qk_norm_rope_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i32, i32, i32, i64, i64, C.c_float, vp]
+    L.mllm_op_qk_norm_rope_bwd_partial_bytes.argtypes = [i64, i32, i32, i32]
+    L.mllm_op_qk_norm_rope_bwd_partial_bytes.restype = sz
+    L.mllm_op_qk_norm_rope_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, i64, i64, i32, i32, i32, i64, i64, i64, C.c_float, vp]
+    L.mllm_op_xent.argtypes = [vp, C.c_int, vp, vp, vp, vp, i64, i32, i32, i64, i64, C.c_float, vp]
     L.mllm_profile_begin.argtypes = [i32]
     L.mllm_profile_end.argtypes = [C.POINTER(i64), C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(i64)]
     dp, ip = C.POINTER(C.c_double), C.POINTER(i32)
@@ -430,6 +441,47 @@ def mllm_op_colsum_static_max_bytes() -> int:
 
 def mllm_op_colsum_static(x, out, accumulate, t, n, stream=None) -> None:
     _check(lib().mllm_op_colsum_static(_ptr(x), _ptr(out), int(accumulate), t, n, _stream(stream)))
+
+
+def mllm_op_embed_fwd(table, ids, y, t, vocab, d, y_stride=None, scale=1.0, table_fp32=0, stream=None) -> None:
+    _check(lib().mllm_op_embed_fwd(_ptr(table), int(table_fp32), _ptr(ids), _ptr(y), t, vocab, d, d if y_stride is None else y_stride,
+                                   scale, _stream(stream)))
+
+
+def mllm_op_embed_bwd_workspace_bytes(t: int, vocab: int, d: int) -> int:
+    return int(lib().mllm_op_embed_bwd_workspace_bytes(t, vocab, d))
+
+
+def mllm_op_embed_bwd(dy, ids, dtable, t, vocab, d, workspace, dy_stride=None, scale=1.0, accumulate=0, stream=None,
+                      workspace_bytes=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else _nbytes(workspace)
+    _check(lib().mllm_op_embed_bwd(_ptr(dy), _ptr(ids), _ptr(dtable), int(accumulate), t, vocab, d, d if dy_stride is None else dy_stride,
+                                   scale, _ptr(workspace), workspace_bytes, _stream(stream)))
+
+
+def mllm_op_qk_norm_rope_fwd(x, gamma_q, gamma_k, y, t, n_q_heads, n_kv_heads, head_dim, x_stride, y_stride, eps, pos=None,
+                             rope_table=None, n_pos=0, stream=None) -> None:
+    _check(lib().mllm_op_qk_norm_rope_fwd(_ptr(x), _ptr(gamma_q), _ptr(gamma_k), _ptr(y), _ptr(pos), _ptr(rope_table), n_pos, t,
+                                          n_q_heads, n_kv_heads, head_dim, x_stride, y_stride, eps, _stream(stream)))
+
+
+def mllm_op_qk_norm_rope_bwd_partial_bytes(t: int, n_q_heads: int, n_kv_heads: int, head_dim: int) -> int:
+    return int(lib().mllm_op_qk_norm_rope_bwd_partial_bytes(t, n_q_heads, n_kv_heads, head_dim))
+
+
+def mllm_op_qk_norm_rope_bwd(dy, x, gamma_q, gamma_k, dx, dgamma_q, dgamma_k, t, n_q_heads, n_kv_heads, head_dim, dy_stride, x_stride,
+                             dx_stride, eps, partial, pos=None, rope_table=None, n_pos=0, accumulate=0, stream=None) -> None:
+    _check(lib().mllm_op_qk_norm_rope_bwd(_ptr(dy), _ptr(x), _ptr(gamma_q), _ptr(gamma_k), _ptr(dx), _ptr(dgamma_q), _ptr(dgamma_k),
+                                          int(accumulate), _ptr(partial), _ptr(pos), _ptr(rope_table), n_pos, t, n_q_heads, n_kv_heads,
+                                          head_dim, dy_stride, x_stride, dx_stride, eps, _stream(stream)))
+
+
+def mllm_op_xent(logits, targets, loss, dlogits, t, vocab, cols, logits_stride=None, dlogits_stride=None, dloss=None, scale=1.0,
+                 logits_fp32=0, stream=None) -> None:
+    _check(lib().mllm_op_xent(_ptr(logits), int(logits_fp32), _ptr(targets), _ptr(dloss), _ptr(loss), _ptr(dlogits), t, vocab, cols,
+                              cols if logits_stride is None else logits_stride, cols if dlogits_stride is None else dlogits_stride,
+                              scale, _stream(stream)))
 
 
 def mllm_profile_begin(max_records: int) -> None:

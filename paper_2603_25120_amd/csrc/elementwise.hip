@@ -920,16 +920,21 @@ int64_t norm_bwd_partial_rows(int64_t t) {
   return t < 1 ? 1 : (t > 1024 ? 1024 : t);
 }
 
-hipError_t PartialSums::take(int64_t rows, int64_t n, std::initializer_list<float*> outs, hipStream_t s, float** partial) {
-  const size_t need = (size_t)rows * (size_t)n * outs.size();
-  bool full = used + need > capacity || count + (int)outs.size() > MAX_JOBS;
+hipError_t PartialSums::room(size_t floats, int64_t n, std::initializer_list<float*> outs, hipStream_t s) {
+  bool full = used + floats > capacity || count + (int)outs.size() > MAX_JOBS;
   for (float* out : outs)
     for (int j = 0; out && j < count; j++) full = full || (out < jobs[j].out + jobs[j].n && jobs[j].out < out + n);
   if (full) {
     hipError_t e = flush(s);
     if (e != hipSuccess) return e;
   }
-  if (need > capacity || (int)outs.size() > MAX_JOBS) return hipErrorInvalidValue;
+  return floats > capacity || (int)outs.size() > MAX_JOBS ? hipErrorInvalidValue : hipSuccess;
+}
+
+hipError_t PartialSums::take(int64_t rows, int64_t n, std::initializer_list<float*> outs, hipStream_t s, float** partial) {
+  const size_t need = (size_t)rows * (size_t)n * outs.size();
+  const hipError_t e = room(need, n, outs, s);
+  if (e != hipSuccess) return e;
   float* p = base + used;
   *partial = p;
   used += need;

@@ -128,6 +128,9 @@ struct PartialSums {
   static constexpr int MAX_JOBS = 32;
   struct Job { const float* partial; float* out; int rows; int64_t n; };
   PartialSums(float* scratch, size_t bytes, int accumulate_) : base(scratch), capacity(bytes / 4), accumulate(accumulate_) {}
+  // Sends off what waits if the next take()s, of this many floats in all for these outputs of n columns, would: afterwards they send
+  // nothing off, so that one kernel may write what several of them took.
+  hipError_t room(size_t floats, int64_t n, std::initializer_list<float*> outs, hipStream_t s);
   hipError_t take(int64_t rows, int64_t n, std::initializer_list<float*> outs, hipStream_t s, float** partial);
   hipError_t flush(hipStream_t s);
   float* base;
@@ -181,6 +184,36 @@ hipError_t launch_unpool_rows(const void* src, void* dst, const int32_t* window,
 // every row of dy.  dx_seq may be dy.
 hipError_t launch_connector_grad(const void* dy, void* dproj, void* dx_seq, const int32_t* rows, const uint32_t* scattered, int64_t n_rows,
                                  int64_t n_seq, int64_t d, hipStream_t s);
+// The token side of a language model (token.hip).
+// y [t, d] (rows y_stride apart, bf16) = scale * table[ids] (bf16, or fp32); ids below 0: zeros, ids not in the table: NaN.
+hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* ids, void* y, int64_t t, int64_t vocab, int64_t d, int64_t y_stride,
+                            float scale, hipStream_t s);
+// dtable [vocab, d] fp32 (+)= scale * the sums of the rows of dy (bf16, dy_stride apart) with the same id; other ids count nowhere.
+size_t embed_bwd_ws_bytes(int64_t t, int64_t vocab, int64_t d);
+hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab, int64_t d, int64_t dy_stride,
+                            float scale, void* ws, hipStream_t s);
+// RMS norm of each of the leading n_q_heads + n_kv_heads heads of a row and, with a rope_table (launch_rope_table, n_pos positions; pos:
+// device int32 [t]), the rotation: x -> y.  Backward: dy -> y, the gradient of x, and the two gains' gradients.
+struct QkNormArgs {
+  const void* x; const void* dy; void* y;
+  const void* gamma_q; const void* gamma_k;      // bf16 [head_dim]
+  const int32_t* pos; const float* rope_table; int64_t n_pos;
+  int64_t t, x_stride, dy_stride, y_stride;
+  int32_t n_q_heads, n_kv_heads, head_dim;       // head_dim a multiple of 16 up to 256
+  float eps;
+};
+hipError_t launch_qk_norm_fwd(const QkNormArgs& a, hipStream_t s);
+size_t qk_norm_bwd_partial_floats(int64_t t, int n_q_heads, int n_kv_heads, int head_dim);   // what launch_qk_norm_bwd takes
+hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamma_k, PartialSums& sums, hipStream_t s);
+// loss [t] = log of the sum over the first vocab columns of exp(logits - logits[target]), 0 where the target is below 0; dlogits (or null)
+// [t, cols] bf16 = scale * dloss * (softmax - one-hot), columns from vocab on 0.
+struct XentArgs {
+  const void* logits; const int32_t* targets; const float* dloss; float* loss; void* dlogits;
+  int64_t t, stride, dstride;
+  int32_t vocab, cols;
+  float scale;
+};
+hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s);
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 
 // Optional per-launch timing with HIP events on the launch stream (off by default).  Classes:

@@ -450,4 +450,120 @@ mllm_status_t mllm_op_colsum_static(const void* x, float* out, int accumulate, i
   return MLLM_OK;
 }
 
+// What the entry points of the token side ask of a matrix: rows that the 16-byte accesses can take.
+static mllm_status_t check_rows(const char* name, const void* p, int64_t width, int64_t stride) {
+  if (stride < width || stride % 8) return op_fail(MLLM_ERR_SHAPE, "%s: row stride below its width or not a multiple of 8", name);
+  if ((uintptr_t)p % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "%s must start on 16 bytes", name);
+  return MLLM_OK;
+}
+#define CHECK(expr)                        \
+  do {                                     \
+    const mllm_status_t r_ = (expr);       \
+    if (r_ != MLLM_OK) return r_;          \
+  } while (0)
+// Counts of rows and of table rows are int32 in the kernels' lists.
+constexpr int64_t MAX_ROWS = INT32_MAX;
+
+static mllm_status_t check_embed(int64_t t, int64_t vocab, int64_t d) {
+  if (t < 0 || t > MAX_ROWS || vocab <= 0 || vocab > MAX_ROWS) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^31 - 1 and vocab in 1 .. 2^31 - 1");
+  if (d <= 0 || d % 8 || d > (1 << 20)) return op_fail(MLLM_ERR_SHAPE, "d must be a positive multiple of 8, at most 2^20");
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_embed_fwd(const void* table, int table_fp32, const int32_t* ids, void* y, int64_t t, int64_t vocab,
+                                int64_t d, int64_t y_stride, float scale, void* hip_stream) {
+  CHECK(check_embed(t, vocab, d));
+  if (!table || (t > 0 && (!ids || !y))) return op_fail(MLLM_ERR_NULL, "table, ids or y is NULL");
+  CHECK(check_rows("table", table, d, d));
+  CHECK(check_rows("y", y, d, y_stride));
+  OP_TRY(launch_embed_fwd(table, table_fp32, ids, y, t, vocab, d, y_stride, scale, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+size_t mllm_op_embed_bwd_workspace_bytes(int64_t t, int64_t vocab, int64_t d) {
+  return t <= 0 || vocab <= 0 || d <= 0 ? 0 : embed_bwd_ws_bytes(t, vocab, d);
+}
+
+mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab,
+                                int64_t d, int64_t dy_stride, float scale, void* workspace, size_t workspace_bytes,
+                                void* hip_stream) {
+  CHECK(check_embed(t, vocab, d));
+  if (!dtable || (t > 0 && (!ids || !dy))) return op_fail(MLLM_ERR_NULL, "dy, ids or dtable is NULL");
+  CHECK(check_rows("dy", dy, d, dy_stride));
+  CHECK(check_rows("dtable", dtable, d, d));
+  const size_t need = mllm_op_embed_bwd_workspace_bytes(t, vocab, d);
+  if (need && !workspace) return op_fail(MLLM_ERR_NULL, "workspace is NULL");
+  if ((uintptr_t)workspace % ALIGN) return op_fail(MLLM_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < need) return op_fail(MLLM_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, need);
+  OP_TRY(launch_embed_bwd(dy, ids, dtable, accumulate, t, vocab, d, dy_stride, scale, workspace, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+// x, the other matrix that is read (the forward pass has none) and the one that is written.
+static mllm_status_t check_qk_norm(const QkNormArgs& a) {
+  if (!a.gamma_q || !a.gamma_k || (a.t > 0 && (!a.x || !a.y || !a.dy))) return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
+  if (a.rope_table && a.t > 0 && !a.pos) return op_fail(MLLM_ERR_NULL, "pos is NULL");
+  if (a.head_dim <= 0 || a.head_dim % 16 || a.head_dim > 256) return op_fail(MLLM_ERR_UNSUPPORTED, "head_dim must be a multiple of 16, at most 256");
+  if (a.n_q_heads <= 0 || a.n_kv_heads <= 0 || a.n_q_heads > 65536 || a.n_kv_heads > 65536)
+    return op_fail(MLLM_ERR_SHAPE, "n_q_heads and n_kv_heads must be positive, at most 65536");
+  const int64_t heads = (int64_t)a.n_q_heads + a.n_kv_heads, width = heads * a.head_dim;
+  if (a.t < 0 || a.t * heads > MAX_ROWS) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, t times the heads below 2^31");
+  if (a.t * width * 2 > ((int64_t)1 << 40)) return op_fail(MLLM_ERR_SHAPE, "more than 2^40 bytes of heads");   // a launch's grid
+  if (!(a.eps >= 0.f)) return op_fail(MLLM_ERR_SHAPE, "eps must not be negative");
+  if (a.rope_table && a.n_pos < 0) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative");
+  CHECK(check_rows("x", a.x, width, a.x_stride));
+  CHECK(check_rows("dy", a.dy, width, a.dy_stride));
+  CHECK(check_rows("the output", a.y, width, a.y_stride));
+  if (((uintptr_t)a.gamma_q | (uintptr_t)a.gamma_k | (uintptr_t)a.rope_table) % 16)
+    return op_fail(MLLM_ERR_UNSUPPORTED, "gamma_q, gamma_k and rope_table must start on 16 bytes");
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const void* gamma_k, void* y, const int32_t* pos,
+                                       const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int64_t x_stride, int64_t y_stride, float eps, void* hip_stream) {
+  const QkNormArgs a = {x, x, y, gamma_q, gamma_k, pos, rope_table, n_pos, t, x_stride, x_stride, y_stride, n_q_heads, n_kv_heads, head_dim, eps};
+  CHECK(check_qk_norm(a));
+  OP_TRY(launch_qk_norm_fwd(a, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+size_t mllm_op_qk_norm_rope_bwd_partial_bytes(int64_t t, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
+  return t < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 ? 0 : qk_norm_bwd_partial_floats(t, n_q_heads, n_kv_heads, head_dim) * 4;
+}
+
+mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void* gamma_q, const void* gamma_k, void* dx,
+                                       float* dgamma_q, float* dgamma_k, int accumulate, float* partial, const int32_t* pos,
+                                       const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
+                                       int32_t head_dim, int64_t dy_stride, int64_t x_stride, int64_t dx_stride, float eps,
+                                       void* hip_stream) {
+  const QkNormArgs a = {x, dy, dx, gamma_q, gamma_k, pos, rope_table, n_pos, t, x_stride, dy_stride, dx_stride, n_q_heads, n_kv_heads, head_dim, eps};
+  if (!dgamma_q || !dgamma_k || !partial) return op_fail(MLLM_ERR_NULL, "dgamma_q, dgamma_k or partial is NULL");
+  CHECK(check_qk_norm(a));
+  if (((uintptr_t)dgamma_q | (uintptr_t)dgamma_k | (uintptr_t)partial) % 16)
+    return op_fail(MLLM_ERR_UNSUPPORTED, "dgamma_q, dgamma_k and partial must start on 16 bytes");
+  PartialSums sums(partial, mllm_op_qk_norm_rope_bwd_partial_bytes(t, n_q_heads, n_kv_heads, head_dim), accumulate);
+  OP_TRY(launch_qk_norm_bwd(a, dgamma_q, dgamma_k, sums, (hipStream_t)hip_stream));
+  OP_TRY(sums.flush((hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* targets, const float* dloss, float* loss,
+                           void* dlogits, int64_t t, int32_t vocab, int32_t cols, int64_t logits_stride, int64_t dlogits_stride,
+                           float scale, void* hip_stream) {
+  if (t < 0 || t > MAX_ROWS) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^31 - 1");
+  if (vocab <= 0 || cols < vocab || cols % 8 || cols > (1 << 30)) return op_fail(MLLM_ERR_SHAPE, "vocab must be in 1 .. cols, cols a multiple of 8, at most 2^30");
+  if (t > 0 && (!logits || !targets || !loss)) return op_fail(MLLM_ERR_NULL, "logits, targets or loss is NULL");
+  CHECK(check_rows("logits", logits, cols, logits_stride));
+  if (dlogits) {
+    CHECK(check_rows("dlogits", dlogits, cols, dlogits_stride));
+    const int64_t in = ((t - 1) * logits_stride + cols) * (logits_fp32 ? 4 : 2), out = ((t - 1) * dlogits_stride + cols) * 2;
+    if (t > 0 && ranges_overlap(logits, in, dlogits, out) && (dlogits != logits || logits_fp32 || dlogits_stride != logits_stride))
+      return op_fail(MLLM_ERR_UNSUPPORTED, "dlogits may be logits (bf16, same stride) but not overlap them otherwise");
+  }
+  const XentArgs a = {logits, targets, dloss, loss, dlogits, t, logits_stride, dlogits_stride, vocab, cols, scale};
+  OP_TRY(launch_xent(a, logits_fp32, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
 }  // extern "C"

@@ -1,0 +1,419 @@
+// The token side of a language model: rows of the token table into the packed sequence and the table's gradient, the RMS norm of
+// every query and key head with the rotary positions in the same pass and its gradient, and the loss over the vocabulary with the
+// gradient of the logits.  All are bound by memory: bf16 (or fp32) storage, fp32 arithmetic, 16-byte accesses, one rounding of each
+// result, no atomics on values that are summed.
+#include <algorithm>
+#include <cmath>
+
+#include "common.h"
+#include "kernels.h"
+
+namespace mllm {
+
+namespace {
+
+__device__ __forceinline__ void unpack8(const uint4& u, float* f) {
+  f[0] = bf16lo(u.x); f[1] = bf16hi(u.x); f[2] = bf16lo(u.y); f[3] = bf16hi(u.y);
+  f[4] = bf16lo(u.z); f[5] = bf16hi(u.z); f[6] = bf16lo(u.w); f[7] = bf16hi(u.w);
+}
+__device__ __forceinline__ uint4 pack8(const float* f) {
+  return make_uint4(pack_bf16x2(f[0], f[1]), pack_bf16x2(f[2], f[3]), pack_bf16x2(f[4], f[5]), pack_bf16x2(f[6], f[7]));
+}
+__device__ __forceinline__ void load8(const float* p, float* f) {
+  const float4 a = *reinterpret_cast<const float4*>(p), b = *reinterpret_cast<const float4*>(p + 4);
+  f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w;
+}
+__device__ __forceinline__ void load8(const bf16_t* p, float* f) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
+
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+constexpr int64_t MAX_GRID = 1 << 20;   // workgroups of a launch; kernels walk on from there
+
+// ---------------------------------------------------------------------------------------------
+// Rows of the token table: y[t] = scale * table[ids[t]], zeros for ids below 0, NaN for ids that the table does not hold.  LPR lanes
+// take a row (of a slice of up to four 16-byte vectors a lane: grid y), so that narrow rows fill the wavefront too.
+// ---------------------------------------------------------------------------------------------
+constexpr int EMBED_VECS = 4;
+template <typename E, int LPR>
+__global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ table, const int32_t* __restrict__ ids, bf16_t* __restrict__ y,
+                                                        int64_t T, int64_t vocab, int nvec, int64_t ldy, float scale) {
+  const int lane = threadIdx.x % LPR, c0 = blockIdx.y * (EMBED_VECS * LPR) + lane;
+  for (int64_t row = (int64_t)blockIdx.x * (256 / LPR) + threadIdx.x / LPR; row < T; row += (int64_t)gridDim.x * (256 / LPR)) {
+    const int32_t id = ids[row];
+    const float nothing = id < 0 ? 0.f : __uint_as_float(0x7fc00000u);
+    const bool there = id >= 0 && id < vocab;
+    const E* src = table + (there ? (int64_t)id * nvec * 8 : 0);
+    float v[EMBED_VECS][8];
+#pragma unroll
+    for (int j = 0; j < EMBED_VECS; j++) {
+      const int c = c0 + j * LPR;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[j][e] = nothing;
+      if (there && c < nvec) load8(src + (int64_t)c * 8, v[j]);
+    }
+#pragma unroll
+    for (int j = 0; j < EMBED_VECS; j++) {
+      const int c = c0 + j * LPR;
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[j][e] *= scale;
+      if (c < nvec) *reinterpret_cast<uint4*>(y + row * ldy + (int64_t)c * 8) = pack8(v[j]);
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// The table's gradient: a workgroup forms one row of the table, going through all tokens.
+// ---------------------------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void embed_bwd_kernel(const bf16_t* __restrict__ dy, const int32_t* __restrict__ ids, float* __restrict__ dtable,
+                                                        int64_t T, int64_t vocab, int nvec, int64_t ld, float scale, int accumulate) {
+  for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x)
+    for (int c = threadIdx.x; c - (int)threadIdx.x < nvec; c += 256) {
+      float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+      bool any = false;
+      for (int64_t t = 0; t < T; t++) {
+        if (ids[t] != v) continue;
+        any = true;
+        float f[8];
+        if (c < nvec) load8(dy + t * ld + (int64_t)c * 8, f);
+        if (c < nvec)
+#pragma unroll
+          for (int e = 0; e < 8; e++) sum[e] += f[e];
+      }
+      if (c >= nvec || (accumulate && !any)) continue;
+      float* o = dtable + (v * nvec + c) * 8;
+#pragma unroll
+      for (int e = 0; e < 8; e++) o[e] = accumulate ? o[e] + scale * sum[e] : scale * sum[e];
+    }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Per-head RMS norm and rotation.  A head is held by LPH lanes, eight of its first half's elements and the eight half-split partners
+// of these in a lane (so the rotation needs no other lane; a head narrower than 16 LPH leaves lanes idle).  A lane group takes up to
+// HEADS heads of a token, so that the rotary factors, twice the bytes of a head's values, are fetched once for all of them.
+// ---------------------------------------------------------------------------------------------
+template <int LPH>
+__device__ __forceinline__ float group_sum(float v) {
+#pragma unroll
+  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+// cos and sin of eight pairs of a row's position; 1 and 0 without a table, NaN for a position outside it.
+__device__ __forceinline__ void rotary_factors(const float* __restrict__ table, const int32_t* __restrict__ pos, int64_t t, int64_t n_pos, int hd,
+                                               int i0, bool active, float* cs, float* sn) {
+#pragma unroll
+  for (int e = 0; e < 8; e++) { cs[e] = 1.f; sn[e] = 0.f; }
+  if (!table) return;
+  const int64_t p = pos[t];
+  if (p < 0 || p >= n_pos) {
+#pragma unroll
+    for (int e = 0; e < 8; e++) cs[e] = sn[e] = __uint_as_float(0x7fc00000u);
+  } else if (active) {
+    load8(table + p * hd + i0, cs);
+    load8(table + p * hd + hd / 2 + i0, sn);
+  }
+}
+
+template <int LPH, int HEADS>
+__global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a, uint32_t units_per_token) {
+  // tokens times lane groups of a token stay below 2^31 (check_qk_norm)
+  const uint32_t unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH, token = unit / units_per_token;
+  const int64_t t = token;
+  if (t >= a.t) return;
+  const int u = (int)(unit - token * units_per_token), i0 = (threadIdx.x % LPH) * 8, half = a.head_dim >> 1;
+  const bool active = i0 < half;
+  const int n_heads = a.n_q_heads + a.n_kv_heads;
+  uint4 lo[HEADS], hi[HEADS];
+#pragma unroll
+  for (int j = 0; j < HEADS; j++) {
+    const int h = u + j * (int)units_per_token;
+    lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
+    if (active && h < n_heads) {
+      const bf16_t* p = (const bf16_t*)a.x + t * a.x_stride + (int64_t)h * a.head_dim + i0;
+      lo[j] = *reinterpret_cast<const uint4*>(p);
+      hi[j] = *reinterpret_cast<const uint4*>(p + half);
+    }
+  }
+  float cs[8], sn[8];
+  rotary_factors(a.rope_table, a.pos, t, a.n_pos, a.head_dim, i0, active, cs, sn);
+#pragma unroll
+  for (int j = 0; j < HEADS; j++) {
+    const int h = u + j * (int)units_per_token;
+    if (h >= n_heads) break;
+    float p[8], q[8], gp[8], gq[8], s = 0.f;
+    unpack8(lo[j], p);
+    unpack8(hi[j], q);
+#pragma unroll
+    for (int e = 0; e < 8; e++) s = fmaf(p[e], p[e], fmaf(q[e], q[e], s));
+    s = group_sum<LPH>(s);
+    if (!active) continue;
+    const float r = rsqrtf(s / (float)a.head_dim + a.eps);
+    const bf16_t* g = (const bf16_t*)(h < a.n_q_heads ? a.gamma_q : a.gamma_k) + i0;
+    load8(g, gp);
+    load8(g + half, gq);
+    float op[8], oq[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const float np = p[e] * r * gp[e], nq = q[e] * r * gq[e];
+      op[e] = a.rope_table ? np * cs[e] - nq * sn[e] : np;
+      oq[e] = a.rope_table ? nq * cs[e] + np * sn[e] : nq;
+    }
+    bf16_t* o = (bf16_t*)a.y + t * a.y_stride + (int64_t)h * a.head_dim + i0;
+    *reinterpret_cast<uint4*>(o) = pack8(op);
+    *reinterpret_cast<uint4*>(o + half) = pack8(oq);
+  }
+}
+
+// Backward: with n = x r and g the gradient of what left the norm (dy turned back), d = g gamma:
+// dx = r (d - n mean(d n)), dgamma = sum over tokens and heads of g n.  r is formed anew from x, which has to be read anyway.  The
+// first q_blocks workgroups take the query heads, the others the key heads, each walking over its share of the tokens with the sums of
+// g n in registers; it leaves one row of partial sums.
+template <int LPH, int HEADS>
+__global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* __restrict__ partial_q, float* __restrict__ partial_k, int q_blocks) {
+  constexpr int GROUPS = 256 / LPH;
+  __shared__ float part[4][LPH][17];
+  const bool is_q = (int)blockIdx.x < q_blocks;
+  const int block = is_q ? blockIdx.x : blockIdx.x - q_blocks, blocks = is_q ? q_blocks : gridDim.x - q_blocks;
+  const int n_heads = is_q ? a.n_q_heads : a.n_kv_heads, col = is_q ? 0 : a.n_q_heads * a.head_dim;
+  const int per_token = (n_heads + HEADS - 1) / HEADS;
+  const int l = threadIdx.x % LPH, i0 = l * 8, half = a.head_dim >> 1;
+  const bool active = i0 < half;
+  float g[16], dg[16];
+#pragma unroll
+  for (int e = 0; e < 16; e++) g[e] = dg[e] = 0.f;
+  if (active) {
+    const bf16_t* gamma = (const bf16_t*)(is_q ? a.gamma_q : a.gamma_k) + i0;
+    load8(gamma, g);
+    load8(gamma + half, g + 8);
+  }
+  const float inv = 1.f / (float)a.head_dim;
+  const uint32_t units = (uint32_t)a.t * per_token;   // below 2^31, as forward
+  for (uint32_t unit = block * GROUPS + threadIdx.x / LPH; unit < units; unit += blocks * GROUPS) {
+    const uint32_t token = unit / (uint32_t)per_token;
+    const int64_t t = token;
+    const int u = (int)(unit - token * per_token);
+    uint4 xl[HEADS], xh[HEADS], dl[HEADS], dh[HEADS];
+#pragma unroll
+    for (int j = 0; j < HEADS; j++) {
+      const int h = u + j * per_token;
+      xl[j] = xh[j] = dl[j] = dh[j] = make_uint4(0, 0, 0, 0);
+      if (active && h < n_heads) {
+        const int64_t c = col + (int64_t)h * a.head_dim + i0;
+        const bf16_t *px = (const bf16_t*)a.x + t * a.x_stride + c, *pd = (const bf16_t*)a.dy + t * a.dy_stride + c;
+        xl[j] = *reinterpret_cast<const uint4*>(px);
+        xh[j] = *reinterpret_cast<const uint4*>(px + half);
+        dl[j] = *reinterpret_cast<const uint4*>(pd);
+        dh[j] = *reinterpret_cast<const uint4*>(pd + half);
+      }
+    }
+    float cs[8], sn[8];
+    rotary_factors(a.rope_table, a.pos, t, a.n_pos, a.head_dim, i0, active, cs, sn);
+#pragma unroll
+    for (int j = 0; j < HEADS; j++) {
+      const int h = u + j * per_token;
+      if (h >= n_heads) break;
+      float x[16], d[16], s = 0.f;
+      unpack8(xl[j], x);
+      unpack8(xh[j], x + 8);
+      unpack8(dl[j], d);
+      unpack8(dh[j], d + 8);
+      if (a.rope_table)
+#pragma unroll
+        for (int e = 0; e < 8; e++) {
+          const float p = d[e], q = d[e + 8];
+          d[e] = p * cs[e] + q * sn[e];
+          d[e + 8] = q * cs[e] - p * sn[e];
+        }
+#pragma unroll
+      for (int e = 0; e < 16; e++) s = fmaf(x[e], x[e], s);
+      const float r = rsqrtf(group_sum<LPH>(s) * inv + a.eps);
+      float m = 0.f;
+#pragma unroll
+      for (int e = 0; e < 16; e++) {
+        x[e] *= r;
+        const float dn = d[e] * x[e];
+        dg[e] += dn;
+        d[e] *= g[e];
+        m = fmaf(dn, g[e], m);
+      }
+      m = group_sum<LPH>(m) * inv;
+      if (!active) continue;
+      float o[16];
+#pragma unroll
+      for (int e = 0; e < 16; e++) o[e] = r * (d[e] - x[e] * m);
+      bf16_t* p = (bf16_t*)a.y + t * a.y_stride + col + (int64_t)h * a.head_dim + i0;
+      *reinterpret_cast<uint4*>(p) = pack8(o);
+      *reinterpret_cast<uint4*>(p + half) = pack8(o + 8);
+    }
+  }
+  // lane groups of a wavefront, then the four wavefronts
+#pragma unroll
+  for (int e = 0; e < 16; e++)
+#pragma unroll
+    for (int o = 32; o >= LPH; o >>= 1) dg[e] += __shfl_xor(dg[e], o, 64);
+  if ((threadIdx.x & 63) < LPH)
+#pragma unroll
+    for (int e = 0; e < 16; e++) part[threadIdx.x >> 6][l][e] = dg[e];
+  __syncthreads();
+  float* out = (is_q ? partial_q : partial_k) + (int64_t)block * a.head_dim;
+  for (int c = threadIdx.x; c < a.head_dim; c += 256) {
+    const int i = c < half ? c : c - half, e = (i & 7) + (c < half ? 0 : 8), k = i >> 3;
+    out[c] = (part[0][k][e] + part[1][k][e]) + (part[2][k][e] + part[3][k][e]);
+  }
+}
+
+// ---------------------------------------------------------------------------------------------
+// Loss over the vocabulary: a workgroup a row, in three passes over it: the maximum, the sum, the gradient.
+// ---------------------------------------------------------------------------------------------
+template <bool MAX>
+__device__ __forceinline__ float block_reduce(float v, float* buf) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) {
+    const float w = __shfl_xor(v, o, 64);
+    v = MAX ? fmaxf(v, w) : v + w;
+  }
+  __syncthreads();
+  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
+  __syncthreads();
+  float r = buf[0];
+  for (int w = 1; w < (int)(blockDim.x >> 6); w++) r = MAX ? fmaxf(r, buf[w]) : r + buf[w];
+  return r;
+}
+template <typename E>
+__global__ __launch_bounds__(256) void xent_kernel(XentArgs a) {
+  __shared__ float buf[4];
+  const int nvec = a.cols >> 3;
+  for (int64_t row = blockIdx.x; row < a.t; row += gridDim.x) {
+    const int32_t target = a.targets[row];
+    const E* x = (const E*)a.logits + row * a.stride;
+    bf16_t* out = a.dlogits ? (bf16_t*)a.dlogits + row * a.dstride : nullptr;
+    if (target < 0) {
+      if (threadIdx.x == 0) a.loss[row] = 0.f;
+      if (out)
+        for (int c = threadIdx.x; c < nvec; c += 256) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
+      continue;
+    }
+    float m = -INFINITY, s = 0.f;
+    for (int c = threadIdx.x; c < nvec; c += 256) {
+      float f[8];
+      load8(x + (int64_t)c * 8, f);
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        if (c * 8 + e < a.vocab) m = fmaxf(m, f[e]);
+    }
+    m = block_reduce<true>(m, buf);
+    for (int c = threadIdx.x; c < nvec; c += 256) {
+      float f[8];
+      load8(x + (int64_t)c * 8, f);
+#pragma unroll
+      for (int e = 0; e < 8; e++)
+        if (c * 8 + e < a.vocab) s += expf(f[e] - m);
+    }
+    if (target >= a.vocab) s = __uint_as_float(0x7fc00000u);
+    s = block_reduce<false>(s, buf);
+    if (threadIdx.x == 0) {
+      float xt[8];
+      const int at = target < a.vocab ? target : 0;
+      load8(x + (at & ~7), xt);
+      a.loss[row] = logf(s) + (m - xt[at & 7]);
+    }
+    if (!out) continue;
+    __syncthreads();                                    // the gradient may be written over the logits
+    const float weight = a.scale * (a.dloss ? a.dloss[row] : 1.f), r = weight / s;
+    for (int c = threadIdx.x; c < nvec; c += 256) {
+      float f[8];
+      load8(x + (int64_t)c * 8, f);
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        const int j = c * 8 + e;
+        f[e] = j < a.vocab ? expf(f[e] - m) * r - (j == target ? weight : 0.f) : 0.f;
+      }
+      *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = pack8(f);
+    }
+  }
+}
+
+}  // namespace
+
+hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* ids, void* y, int64_t t, int64_t vocab, int64_t d, int64_t y_stride,
+                            float scale, hipStream_t s) {
+  if (t == 0) return hipSuccess;
+  const int nvec = (int)(d / 8), lpr = nvec <= 8 ? 8 : nvec <= 16 ? 16 : nvec <= 32 ? 32 : 64;
+  const dim3 grid((unsigned)std::min<int64_t>(ceil_div(t, 256 / lpr), MAX_GRID), (unsigned)ceil_div(nvec, EMBED_VECS * lpr));
+  ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * (table_fp32 ? 6.0 : 4.0), s);
+#define CALL(E, L) hipLaunchKernelGGL((embed_fwd_kernel<E, L>), grid, dim3(256), 0, s, (const E*)table, ids, (bf16_t*)y, t, vocab, nvec, y_stride, scale)
+#define CALL_LPR(E) \
+  do { if (lpr == 8) CALL(E, 8); else if (lpr == 16) CALL(E, 16); else if (lpr == 32) CALL(E, 32); else CALL(E, 64); } while (0)
+  if (table_fp32) CALL_LPR(float); else CALL_LPR(bf16_t);
+#undef CALL_LPR
+#undef CALL
+  return hipGetLastError();
+}
+
+size_t embed_bwd_ws_bytes(int64_t t, int64_t vocab, int64_t d) { return 0; }
+
+hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab, int64_t d, int64_t dy_stride,
+                            float scale, void* ws, hipStream_t s) {
+  ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0 + (accumulate ? 0.0 : (double)vocab * (double)d * 4.0), s);
+  hipLaunchKernelGGL(embed_bwd_kernel, dim3((unsigned)std::min<int64_t>(vocab, MAX_GRID)), dim3(256), 0, s, (const bf16_t*)dy, ids, dtable, t, vocab,
+                     (int)(d / 8), dy_stride, scale, accumulate);
+  return hipGetLastError();
+}
+
+namespace {
+constexpr int QK_HEADS = 4;
+int qk_lanes(int head_dim) { return head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
+// Workgroups of the backward pass that take `heads` of `all` heads.
+int64_t qk_bwd_blocks(int64_t t, int heads, int all, int head_dim) {
+  const int64_t units = t * ceil_div(heads, QK_HEADS), groups = 256 / qk_lanes(head_dim);
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), ceil_div((int64_t)1024 * heads, all)));
+}
+}  // namespace
+
+hipError_t launch_qk_norm_fwd(const QkNormArgs& a, hipStream_t s) {
+  if (a.t == 0) return hipSuccess;
+  const int n_heads = a.n_q_heads + a.n_kv_heads, units = (int)ceil_div(n_heads, QK_HEADS), lph = qk_lanes(a.head_dim);
+  ProfScope prof(PROF_ELEMENTWISE, 4.0 * (double)a.t * n_heads * a.head_dim, s);
+  const dim3 grid((unsigned)ceil_div(a.t * units, 256 / lph));
+#define CALL(L) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, QK_HEADS>), grid, dim3(256), 0, s, a, units)
+  if (lph == 2) CALL(2); else if (lph == 4) CALL(4); else if (lph == 8) CALL(8); else CALL(16);
+#undef CALL
+  return hipGetLastError();
+}
+
+size_t qk_norm_bwd_partial_floats(int64_t t, int n_q_heads, int n_kv_heads, int head_dim) {
+  const int all = n_q_heads + n_kv_heads;
+  return (size_t)((qk_bwd_blocks(t, n_q_heads, all, head_dim) + qk_bwd_blocks(t, n_kv_heads, all, head_dim)) * head_dim);
+}
+
+hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamma_k, PartialSums& sums, hipStream_t s) {
+  const int all = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
+  const int64_t bq = qk_bwd_blocks(a.t, a.n_q_heads, all, a.head_dim), bk = qk_bwd_blocks(a.t, a.n_kv_heads, all, a.head_dim);
+  float *pq = nullptr, *pk = nullptr;
+  ProfScope prof(PROF_ELEMENTWISE, 6.0 * (double)a.t * all * a.head_dim, s);
+#define CALL(L, BLOCKS, Q) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q))
+#define CALL_LPH(BLOCKS, Q) \
+  do { if (lph == 2) CALL(2, BLOCKS, Q); else if (lph == 4) CALL(4, BLOCKS, Q); else if (lph == 8) CALL(8, BLOCKS, Q); else CALL(16, BLOCKS, Q); } while (0)
+  hipError_t e = sums.room((size_t)(bq + bk) * a.head_dim, a.head_dim, {dgamma_q, dgamma_k}, s);
+  if (e == hipSuccess) e = sums.take(bq, a.head_dim, {dgamma_q}, s, &pq);
+  if (e != hipSuccess) return e;
+  const int64_t bytes = (int64_t)a.head_dim * 4;
+  const bool shared = ranges_overlap(dgamma_q, bytes, dgamma_k, bytes);   // then the second take sends the first sums off
+  if (shared) CALL_LPH(bq, bq);
+  if ((e = sums.take(bk, a.head_dim, {dgamma_k}, s, &pk)) != hipSuccess) return e;
+  if (shared) CALL_LPH(bk, 0); else CALL_LPH(bq + bk, bq);
+#undef CALL_LPH
+#undef CALL
+  return hipGetLastError();
+}
+
+hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
+  if (a.t == 0) return hipSuccess;
+  ProfScope prof(PROF_ELEMENTWISE, (double)a.t * ((logits_fp32 ? 4.0 : 2.0) * (double)a.vocab + (a.dlogits ? 2.0 * (double)a.cols : 0.0)), s);
+  const dim3 grid((unsigned)std::min<int64_t>(a.t, MAX_GRID));
+  if (logits_fp32)
+    hipLaunchKernelGGL(xent_kernel<float>, grid, dim3(256), 0, s, a);
+  else
+    hipLaunchKernelGGL(xent_kernel<bf16_t>, grid, dim3(256), 0, s, a);
+  return hipGetLastError();
+}
+
+}  // namespace mllm
