@@ -461,11 +461,11 @@ static mllm_status_t check_rows(const char* name, const void* p, int64_t width, 
     const mllm_status_t r_ = (expr);       \
     if (r_ != MLLM_OK) return r_;          \
   } while (0)
-// Counts of rows and of table rows are int32 in the kernels' lists.
+// Rows are counted in int32 in the kernels' lists.
 constexpr int64_t MAX_ROWS = INT32_MAX;
 
 static mllm_status_t check_embed(int64_t t, int64_t vocab, int64_t d) {
-  if (t < 0 || t > MAX_ROWS || vocab <= 0 || vocab > MAX_ROWS) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^31 - 1 and vocab in 1 .. 2^31 - 1");
+  if (t < 0 || t > MAX_ROWS || vocab <= 0 || vocab > (1 << 30)) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^31 - 1 and vocab in 1 .. 2^30");
   if (d <= 0 || d % 8 || d > (1 << 20)) return op_fail(MLLM_ERR_SHAPE, "d must be a positive multiple of 8, at most 2^20");
   return MLLM_OK;
 }

@@ -61,28 +61,198 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ ta
 }
 
 // ---------------------------------------------------------------------------------------------
-// The table's gradient: a workgroup forms one row of the table, going through all tokens.
+// The table's gradient.  The tokens are first brought together by id (embed_sort_kernel), then chunks of the sorted tokens are added up,
+// every chunk alike long whatever the ids' frequencies (embed_sum_kernel); ids that go on beyond their chunk leave partial sums, which
+// embed_join_kernel adds up chunk after chunk.  All orders are those of the tokens: no atomics on sums, same bits every time.
+//
+// Sorting: ids are dealt to `buckets` (a power of two, at least 256, at most 1024 ids each) by their lowest bits, so that frequent
+// neighbours land in different ones.  A workgroup owns a bucket and reads ALL ids: those of lower buckets only count, which gives its place
+// in the list without waiting for any other workgroup.  Each of its 16 wavefronts counts a contiguous piece of the tokens per
+// id; from the scan over (id, wavefront) it then places its piece's tokens in their order.  The ids come from L2: 32768 of them are 128 KB.
+// With the gradient overwritten, the workgroup that knows which rows of its bucket nobody asked for clears them.
 // ---------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void embed_bwd_kernel(const bf16_t* __restrict__ dy, const int32_t* __restrict__ ids, float* __restrict__ dtable,
-                                                        int64_t T, int64_t vocab, int nvec, int64_t ld, float scale, int accumulate) {
-  for (int64_t v = blockIdx.x; v < vocab; v += gridDim.x)
-    for (int c = threadIdx.x; c - (int)threadIdx.x < nvec; c += 256) {
-      float sum[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-      bool any = false;
-      for (int64_t t = 0; t < T; t++) {
-        if (ids[t] != v) continue;
-        any = true;
-        float f[8];
-        if (c < nvec) load8(dy + t * ld + (int64_t)c * 8, f);
-        if (c < nvec)
+constexpr int SORT_WAVES = 16, SORT_RANGE = 1024;   // ids a bucket holds at most
+__device__ __forceinline__ int lanes_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); }
+
+__global__ __launch_bounds__(64 * SORT_WAVES) void embed_sort_kernel(const int32_t* __restrict__ ids, int T, int vocab, int log2_buckets, int nvec,
+                                                                     int32_t* __restrict__ order, int32_t* __restrict__ keys, int32_t* __restrict__ total,
+                                                                     float* __restrict__ dtable, int clear) {
+  __shared__ int hist[SORT_WAVES][SORT_RANGE];
+  __shared__ int sums[SORT_WAVES], below_of[SORT_WAVES];
+  __shared__ uint64_t empty[SORT_WAVES];
+  const int bucket = blockIdx.x, mask = (1 << log2_buckets) - 1, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int range = (vocab - bucket + mask) >> log2_buckets;   // ids bucket, bucket + buckets, ... below vocab
+  for (int i = threadIdx.x; i < range; i += 64 * SORT_WAVES)
 #pragma unroll
-          for (int e = 0; e < 8; e++) sum[e] += f[e];
-      }
-      if (c >= nvec || (accumulate && !any)) continue;
-      float* o = dtable + (v * nvec + c) * 8;
+    for (int w = 0; w < SORT_WAVES; w++) hist[w][i] = 0;
+  __syncthreads();
+  const int piece = (int)(((int64_t)T + 64 * SORT_WAVES - 1) / (64 * SORT_WAVES) * 64);
+  const int64_t first = (int64_t)wave * piece, end = first + piece < T ? first + piece : T;
+  constexpr int AHEAD = 8;
+  int below = 0;
+  for (int64_t t0 = first; t0 < end; t0 += 64 * AHEAD) {
+    int32_t id[AHEAD];
 #pragma unroll
-      for (int e = 0; e < 8; e++) o[e] = accumulate ? o[e] + scale * sum[e] : scale * sum[e];
+    for (int j = 0; j < AHEAD; j++) id[j] = t0 + 64 * j + lane < end ? ids[t0 + 64 * j + lane] : -1;
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      const bool there = (uint32_t)id[j] < (uint32_t)vocab;
+      below += there && (id[j] & mask) < bucket;
+      if (there && (id[j] & mask) == bucket) atomicAdd(&hist[wave][id[j] >> log2_buckets], 1);
     }
+  }
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) below += __shfl_xor(below, o, 64);
+  if (lane == 0) below_of[wave] = below;
+  __syncthreads();
+  // the scan: thread i has the i-th id of the bucket
+  int count = 0;
+  if (threadIdx.x < range)
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; w++) count += hist[w][threadIdx.x];
+  int upto = count;
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) {
+    const int v = __shfl_up(upto, o, 64);
+    if (lane >= o) upto += v;
+  }
+  if (lane == 63) sums[wave] = upto;
+  __syncthreads();
+  int at = upto - count;
+#pragma unroll
+  for (int w = 0; w < SORT_WAVES; w++) at += below_of[w] + (w < wave ? sums[w] : 0);
+  if (T > 0 && bucket == mask && threadIdx.x == 64 * SORT_WAVES - 1) *total = at + count;
+  if (threadIdx.x < range)
+#pragma unroll
+    for (int w = 0; w < SORT_WAVES; w++) {
+      const int n = hist[w][threadIdx.x];
+      hist[w][threadIdx.x] = at;
+      at += n;
+    }
+  const uint64_t without = __ballot(threadIdx.x < range && count == 0);
+  if (lane == 0) empty[wave] = without;
+  __syncthreads();
+  if (clear)
+    for (int i = wave; i < range; i += SORT_WAVES) {
+      if (!(empty[i >> 6] >> (i & 63) & 1)) continue;
+      float4* row = reinterpret_cast<float4*>(dtable + (((int64_t)i << log2_buckets) + bucket) * nvec * 8);
+      for (int c = lane; c < 2 * nvec; c += 64) row[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  for (int64_t t0 = first; t0 < end; t0 += 64 * AHEAD) {
+    int32_t id[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) id[j] = t0 + 64 * j + lane < end ? ids[t0 + 64 * j + lane] : -1;
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      const bool mine = (uint32_t)id[j] < (uint32_t)vocab && (id[j] & mask) == bucket;
+      uint64_t left = __ballot(mine);
+      while (left) {   // the lanes of one id at a time
+        const int32_t v = __builtin_amdgcn_readlane(id[j], __builtin_ctzll(left));
+        const uint64_t same = __ballot(mine && id[j] == v);
+        int place = 0;
+        if (lane == 0) place = atomicAdd(&hist[wave][v >> log2_buckets], __popcll(same));
+        place = __builtin_amdgcn_readfirstlane(place) + lanes_below(same);
+        if (mine && id[j] == v) {
+          order[place] = (int32_t)(t0 + 64 * j + lane);
+          keys[place] = v;
+        }
+        left &= ~same;
+      }
+    }
+  }
+}
+
+// Adds up a chunk of the sorted tokens: LPR lanes take eight columns each (of a slice of 8 LPR columns) and walk over the chunk's rows, eight
+// requested at a time; where the id changes, the sum goes to its row of the table.  A sum whose id began in an earlier chunk, or goes
+// on in the next one, goes to the partial sums instead: [0][chunk] or [1][chunk].
+template <int LPR>
+__global__ __launch_bounds__(256) void embed_sum_kernel(const bf16_t* __restrict__ dy, const int32_t* __restrict__ order, const int32_t* __restrict__ keys,
+                                                        const int32_t* __restrict__ total, float* __restrict__ dtable, float* __restrict__ partial,
+                                                        int chunk, int n_chunks, int slices, int nvec, int64_t ld, float scale, int accumulate) {
+  constexpr int AHEAD = 8;
+  const uint32_t item = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
+  const int c = (int)(item / (uint32_t)slices), v = (int)(item - (uint32_t)c * slices) * LPR + threadIdx.x % LPR;
+  const int N = *total;
+  const int64_t p0 = (int64_t)c * chunk;
+  if (c >= n_chunks || p0 >= N || v >= nvec) return;
+  const int n = N - p0 < chunk ? (int)(N - p0) : chunk;
+  int32_t cur = keys[p0];
+  bool began_before = c > 0 && keys[p0 - 1] == cur;
+  const bool more = p0 + n < N;
+  const int32_t next = more ? keys[p0 + n] : 0;
+  const bf16_t* src = dy + (int64_t)v * 8;
+  float acc[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  auto put = [&](int slot) {   // slot 0, 1: partial sums; 2: the table
+    float* o = slot < 2 ? partial + (((int64_t)slot * n_chunks + c) * nvec + v) * 8 : dtable + ((int64_t)cur * nvec + v) * 8;
+    float f[8];
+    if (slot == 2 && accumulate) load8(o, f);
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = slot < 2 ? acc[e] : accumulate ? fmaf(scale, acc[e], f[e]) : scale * acc[e];
+    reinterpret_cast<float4*>(o)[0] = make_float4(f[0], f[1], f[2], f[3]);
+    reinterpret_cast<float4*>(o)[1] = make_float4(f[4], f[5], f[6], f[7]);
+  };
+  for (int i = 0; i < n; i += AHEAD) {
+    int32_t key[AHEAD];
+    uint4 row[AHEAD];
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      const int64_t p = p0 + (i + j < n ? i + j : n - 1);   // the last rows again where there are no more
+      key[j] = keys[p];
+      row[j] = *reinterpret_cast<const uint4*>(src + order[p] * ld);
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      if (i + j >= n) break;
+      if (key[j] != cur) {
+        put(began_before ? 0 : 2);
+        began_before = false;
+        cur = key[j];
+#pragma unroll
+        for (int e = 0; e < 8; e++) acc[e] = 0.f;
+      }
+      float f[8];
+      unpack8(row[j], f);
+#pragma unroll
+      for (int e = 0; e < 8; e++) acc[e] += f[e];
+    }
+  }
+  put(began_before ? 0 : more && next == cur ? 1 : 2);
+}
+
+// An id that begins in chunk c and goes on beyond it: its last partial sum of that chunk and the first ones of the following chunks, as
+// many as begin with it.  A wavefront has 256 columns.
+__global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restrict__ keys, const int32_t* __restrict__ total, float* __restrict__ dtable,
+                                                         const float* __restrict__ partial, int chunk, int n_chunks, int slices, int nvec, float scale,
+                                                         int accumulate) {
+  const uint32_t item = blockIdx.x * 4 + (threadIdx.x >> 6);
+  const int c = (int)(item / (uint32_t)slices), lane = threadIdx.x & 63, q = (int)(item - (uint32_t)c * slices) * 64 + lane;   // q: four columns
+  const int N = *total;
+  const int64_t p0 = (int64_t)c * chunk, p1 = p0 + chunk;
+  if (c >= n_chunks || p1 >= N) return;
+  const int32_t id = keys[p1 - 1];
+  if (keys[p1] != id || (c > 0 && keys[p0] == id && keys[p0 - 1] == id)) return;
+  int chunks = 1;                                    // that begin with the id
+  while (true) {
+    const int64_t p = p1 + (int64_t)(chunks + lane) * chunk;
+    const uint64_t others = ~__ballot(p < N && keys[p] == id);
+    if (others) { chunks += __builtin_ctzll(others); break; }
+    chunks += 64;
+  }
+  if (q >= 2 * nvec) return;
+  const int64_t step = (int64_t)nvec * 2;
+  const float4* src = reinterpret_cast<const float4*>(partial) + q;
+  float4 sum = src[((int64_t)n_chunks + c) * step];
+  src += (int64_t)(c + 1) * step;
+  for (int i = 0; i < chunks; i += 8) {
+    float4 f[8];
+#pragma unroll
+    for (int j = 0; j < 8; j++) f[j] = i + j < chunks ? src[(int64_t)(i + j) * step] : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+    for (int j = 0; j < 8; j++) { sum.x += f[j].x; sum.y += f[j].y; sum.z += f[j].z; sum.w += f[j].w; }
+  }
+  float4* o = reinterpret_cast<float4*>(dtable) + (int64_t)id * step + q;
+  float4 old = accumulate ? *o : make_float4(0.f, 0.f, 0.f, 0.f);
+  *o = make_float4(fmaf(scale, sum.x, old.x), fmaf(scale, sum.y, old.y), fmaf(scale, sum.z, old.z), fmaf(scale, sum.w, old.w));
 }
 
 // ---------------------------------------------------------------------------------------------
@@ -348,13 +518,59 @@ hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* id
   return hipGetLastError();
 }
 
-size_t embed_bwd_ws_bytes(int64_t t, int64_t vocab, int64_t d) { return 0; }
+namespace {
+// How the sorted tokens are cut: into chunks of 8, 16 or 32, the shortest that make at most 8192 wavefronts (32 a CU).
+struct EmbedCut { int lpr, slices, chunk; int64_t chunks; };
+EmbedCut embed_cut(int64_t t, int64_t d) {
+  EmbedCut c;
+  const int nvec = (int)(d / 8);
+  c.lpr = nvec <= 8 ? 8 : nvec <= 16 ? 16 : nvec <= 32 ? 32 : 64;
+  c.slices = (int)ceil_div(nvec, c.lpr);
+  c.chunk = 8;
+  while (c.chunk < 32 && ceil_div(t, c.chunk) * c.slices * c.lpr > 8192 * 64) c.chunk *= 2;
+  c.chunks = ceil_div(t, c.chunk);
+  return c;
+}
+size_t align256(size_t n) { return (n + 255) / 256 * 256; }
+}  // namespace
+
+// The token order, its ids, their number; two rows of partial sums a chunk.  Not less for fewer tokens: shorter chunks are never more
+// than 8192 wavefronts' worth.
+size_t embed_bwd_ws_bytes(int64_t t, int64_t vocab, int64_t d) {
+  const EmbedCut c = embed_cut(t, d);
+  const int64_t most = std::max(ceil_div(t, 32), std::min<int64_t>(ceil_div(t, 8), 8192 * 64 / c.lpr / c.slices));
+  return 2 * align256((size_t)t * 4) + 256 + (size_t)2 * most * d * 4;
+}
 
 hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab, int64_t d, int64_t dy_stride,
                             float scale, void* ws, hipStream_t s) {
-  ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0 + (accumulate ? 0.0 : (double)vocab * (double)d * 4.0), s);
-  hipLaunchKernelGGL(embed_bwd_kernel, dim3((unsigned)std::min<int64_t>(vocab, MAX_GRID)), dim3(256), 0, s, (const bf16_t*)dy, ids, dtable, t, vocab,
-                     (int)(d / 8), dy_stride, scale, accumulate);
+  if (t == 0 && accumulate) return hipSuccess;   // without tokens the sorting kernel only clears
+  const EmbedCut c = embed_cut(t, d);
+  const int nvec = (int)(d / 8);
+  int log2_buckets = 8;
+  while (ceil_div(vocab, (int64_t)1 << log2_buckets) > SORT_RANGE) log2_buckets++;
+  char* w = (char*)ws;
+  int32_t *order = (int32_t*)w, *keys = (int32_t*)(w + align256((size_t)t * 4)), *total = (int32_t*)(w + 2 * align256((size_t)t * 4));
+  float* partial = (float*)((char*)total + 256);
+  {
+    ProfScope prof(PROF_ELEMENTWISE, accumulate ? 0.0 : (double)vocab * (double)d * 4.0, s);
+    hipLaunchKernelGGL(embed_sort_kernel, dim3(1u << log2_buckets), dim3(64 * SORT_WAVES), 0, s, ids, (int)t, (int)vocab, log2_buckets, nvec, order, keys,
+                       total, dtable, accumulate ? 0 : 1);
+  }
+  if (t == 0) return hipGetLastError();
+  {
+    ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0, s);
+    const dim3 grid((unsigned)ceil_div(c.chunks * c.slices, 256 / c.lpr));
+#define CALL(L)                                                                                                                                  \
+  hipLaunchKernelGGL((embed_sum_kernel<L>), grid, dim3(256), 0, s, (const bf16_t*)dy, order, keys, total, dtable, partial, c.chunk, (int)c.chunks, \
+                     c.slices, nvec, dy_stride, scale, accumulate)
+    if (c.lpr == 8) CALL(8); else if (c.lpr == 16) CALL(16); else if (c.lpr == 32) CALL(32); else CALL(64);
+#undef CALL
+  }
+  ProfScope prof(PROF_ELEMENTWISE, 0.0, s);
+  const int slices = (int)ceil_div(nvec, 32);
+  hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)ceil_div(c.chunks * slices, 4)), dim3(256), 0, s, keys, total, dtable, partial, c.chunk,
+                     (int)c.chunks, slices, nvec, scale, accumulate);
   return hipGetLastError();
 }
 

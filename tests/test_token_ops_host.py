@@ -35,16 +35,24 @@ def test_embed_fwd_refusals(B, status, change):
 
 
 @pytest.mark.parametrize("status,change", [
-    (NULL, dict(dy=None)), (NULL, dict(ids=None)), (NULL, dict(dtable=None)),
+    (NULL, dict(dy=None)), (NULL, dict(ids=None)), (NULL, dict(dtable=None)), (NULL, dict(workspace=None)),
     (SHAPE, dict(t=-1)), (SHAPE, dict(vocab=0)), (SHAPE, dict(d=60)), (SHAPE, dict(dy_stride=56)), (SHAPE, dict(dy_stride=65)),
     (UNSUPPORTED, dict(dy=P + 8)), (UNSUPPORTED, dict(dtable=P + 4)),
-    (WORKSPACE, dict(workspace=P + 16)),
+    (WORKSPACE, dict(workspace=P + 16)), (WORKSPACE, dict(short=1)),
 ])
 def test_embed_bwd_refusals(B, status, change):
     need = B.mllm_op_embed_bwd_workspace_bytes(4, 10, 64)
     kw = {**dict(dy=P, ids=P, dtable=P, t=4, vocab=10, d=64, workspace=P, workspace_bytes=need), **change}
     kw["workspace_bytes"] -= kw.pop("short", 0)
     refused(B, status, B.mllm_op_embed_bwd, **kw)
+
+
+def test_embed_bwd_workspace_serves_fewer_tokens(B):
+    """One buffer sized for the longest microbatch serves every shorter one."""
+    for vocab, d in ((10, 64), (50257, 3584), (131072, 4096), (1000000, 8)):
+        sizes = [B.mllm_op_embed_bwd_workspace_bytes(t, vocab, d) for t in (0, 1, 2, 31, 64, 65, 1000, 5000, 32768, 1000000)]
+        assert sizes == sorted(sizes) and sizes[0] == 0 and sizes[1] > 0
+    assert B.mllm_op_embed_bwd_workspace_bytes(-1, 10, 64) == 0 and B.mllm_op_embed_bwd_workspace_bytes(4, 0, 64) == 0
 
 
 QK = dict(x=P, gamma_q=P, gamma_k=P, t=4, n_q_heads=4, n_kv_heads=2, head_dim=64, x_stride=512, eps=1e-6, pos=P, rope_table=P, n_pos=8)
