@@ -26,7 +26,7 @@ __device__ __forceinline__ void load8(const float* p, float* f) {
 __device__ __forceinline__ void load8(const bf16_t* p, float* f) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
-constexpr int64_t MAX_GRID = 1 << 20;   // workgroups of a launch; kernels walk on from there
+constexpr int64_t MAX_GRID = 1 << 20;   // workgroups along x: a dimension holds fewer than 2^32 threads
 
 // ---------------------------------------------------------------------------------------------
 // Rows of the token table: y[t] = scale * table[ids[t]], zeros for ids below 0, NaN for ids that the table does not hold.  LPR lanes
@@ -431,74 +431,182 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
 }
 
 // ---------------------------------------------------------------------------------------------
-// Loss over the vocabulary: a workgroup a row, in three passes over it: the maximum, the sum, the gradient.
+// Loss over the vocabulary and its gradient, the row read once: GROUP threads hold up to NV vectors of eight logits each in registers
+// from the maximum to the gradient; what a longer row has beyond GROUP * NV vectors is read again for the gradient.  With the
+// maximum m and L = log2(e):  s = sum 2^((x - m) L), loss = log2(s) / L + (m - x[target]), gradient = 2^((x - m) L - log2(s) + log2 |weight|)
+// with the weight's sign, less the weight at the target.  Every thread sums against its own maximum, so that one exchange joins (m, s) of all.
+// (x L - m L in one instruction would lose rows of the type's lowest value: m L is beyond the largest number.)
 // ---------------------------------------------------------------------------------------------
-template <bool MAX>
-__device__ __forceinline__ float block_reduce(float v, float* buf) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) {
-    const float w = __shfl_xor(v, o, 64);
-    v = MAX ? fmaxf(v, w) : v + w;
-  }
-  __syncthreads();
-  if ((threadIdx.x & 63) == 0) buf[threadIdx.x >> 6] = v;
-  __syncthreads();
-  float r = buf[0];
-  for (int w = 1; w < (int)(blockDim.x >> 6); w++) r = MAX ? fmaxf(r, buf[w]) : r + buf[w];
-  return r;
-}
+constexpr float LOG2E = 1.4426950408889634f;
+typedef short s16x2 __attribute__((ext_vector_type(2)));
+typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
+
 template <typename E>
-__global__ __launch_bounds__(256) void xent_kernel(XentArgs a) {
-  __shared__ float buf[4];
-  const int nvec = a.cols >> 3;
-  for (int64_t row = blockIdx.x; row < a.t; row += gridDim.x) {
-    const int32_t target = a.targets[row];
-    const E* x = (const E*)a.logits + row * a.stride;
-    bf16_t* out = a.dlogits ? (bf16_t*)a.dlogits + row * a.dstride : nullptr;
-    if (target < 0) {
-      if (threadIdx.x == 0) a.loss[row] = 0.f;
-      if (out)
-        for (int c = threadIdx.x; c < nvec; c += 256) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
-      continue;
-    }
-    float m = -INFINITY, s = 0.f;
-    for (int c = threadIdx.x; c < nvec; c += 256) {
-      float f[8];
-      load8(x + (int64_t)c * 8, f);
+struct Logits8;
+template <>
+struct Logits8<bf16_t> {
+  uint4 u;
+  __device__ __forceinline__ void load(const bf16_t* p) { u = *reinterpret_cast<const uint4*>(p); }
+  __device__ __forceinline__ void none() { u = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }   // -inf
+  __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
+  // Keeps the compiler from carrying the unpacked values from one use to the next (129 registers spilled with 16 vectors).
+  __device__ __forceinline__ void settle() { asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
+  __device__ __forceinline__ void keep(int n) {   // the first n, 1 to 7
+    uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-      for (int e = 0; e < 8; e++)
-        if (c * 8 + e < a.vocab) m = fmaxf(m, f[e]);
-    }
-    m = block_reduce<true>(m, buf);
-    for (int c = threadIdx.x; c < nvec; c += 256) {
-      float f[8];
-      load8(x + (int64_t)c * 8, f);
+    for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? (w[i] & 0xffffu) | 0xff800000u : 0xff80ff80u;
+    u = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <>
+struct Logits8<float> {
+  float4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
+  __device__ __forceinline__ void none() { a = b = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); }
+  __device__ __forceinline__ void settle() {}
+  __device__ __forceinline__ void get(float* f) const { f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w; }
+  __device__ __forceinline__ void keep(int n) {
+    float f[8];
+    get(f);
 #pragma unroll
-      for (int e = 0; e < 8; e++)
-        if (c * 8 + e < a.vocab) s += expf(f[e] - m);
-    }
-    if (target >= a.vocab) s = __uint_as_float(0x7fc00000u);
-    s = block_reduce<false>(s, buf);
-    if (threadIdx.x == 0) {
-      float xt[8];
-      const int at = target < a.vocab ? target : 0;
-      load8(x + (at & ~7), xt);
-      a.loss[row] = logf(s) + (m - xt[at & 7]);
-    }
-    if (!out) continue;
-    __syncthreads();                                    // the gradient may be written over the logits
-    const float weight = a.scale * (a.dloss ? a.dloss[row] : 1.f), r = weight / s;
-    for (int c = threadIdx.x; c < nvec; c += 256) {
-      float f[8];
-      load8(x + (int64_t)c * 8, f);
+    for (int i = 0; i < 8; i++) f[i] = i < n ? f[i] : -INFINITY;
+    a = make_float4(f[0], f[1], f[2], f[3]);
+    b = make_float4(f[4], f[5], f[6], f[7]);
+  }
+};
+// The largest of N vectors.  bf16 in pairs without unpacking: among 16-bit integers numbers at or above zero keep their order and are
+// above all others; where there are none, the largest is the smallest unsigned one.
+template <int N>
+__device__ __forceinline__ float largest(const Logits8<bf16_t>* v) {
+  s16x2 m = {-32768, -32768};
 #pragma unroll
-      for (int e = 0; e < 8; e++) {
-        const int j = c * 8 + e;
-        f[e] = j < a.vocab ? expf(f[e] - m) * r - (j == target ? weight : 0.f) : 0.f;
-      }
-      *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = pack8(f);
+  for (int j = 0; j < N; j++)
+    for (uint32_t w : {v[j].u.x, v[j].u.y, v[j].u.z, v[j].u.w}) m = __builtin_elementwise_max(m, __builtin_bit_cast(s16x2, w));
+  uint32_t top = (uint16_t)(m[0] > m[1] ? m[0] : m[1]);
+  if (top & 0x8000u) {
+    u16x2 n = {65535, 65535};
+#pragma unroll
+    for (int j = 0; j < N; j++)
+      for (uint32_t w : {v[j].u.x, v[j].u.y, v[j].u.z, v[j].u.w}) n = __builtin_elementwise_min(n, __builtin_bit_cast(u16x2, w));
+    top = n[0] < n[1] ? n[0] : n[1];
+  }
+  return __uint_as_float(top << 16);
+}
+template <int N>
+__device__ __forceinline__ float largest(const Logits8<float>* v) {
+  float m = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < N; j++) m = fmaxf(fmaxf(fmaxf(fmaxf(v[j].a.x, v[j].a.y), fmaxf(v[j].a.z, v[j].a.w)), fmaxf(fmaxf(v[j].b.x, v[j].b.y), fmaxf(v[j].b.z, v[j].b.w))), m);
+  return m;
+}
+
+// What a sum against the maximum `from` is worth against `to`, at or above it; a sum of nothing but -inf is none.
+__device__ __forceinline__ float rescale(float from, float to) { return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * LOG2E); }
+
+template <typename E, int GROUP, int NV>
+__global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArgs a) {
+  constexpr int BLOCK = GROUP < 256 ? 256 : GROUP, WAVES = GROUP / 64;
+  __shared__ float2 wave_sums[WAVES];
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (BLOCK / GROUP) + threadIdx.x / GROUP;
+  if (row >= a.t) return;                              // the whole group
+  const int tid = threadIdx.x % GROUP, nvec = (a.vocab + 7) >> 3, tail = a.vocab & 7;
+  const int32_t target = a.targets[row];
+  const E* x = (const E*)a.logits + row * a.stride;
+  bf16_t* out = a.dlogits ? (bf16_t*)a.dlogits + row * a.dstride : nullptr;
+  if (target < 0) {
+    if (tid == 0) a.loss[row] = 0.f;
+    if (out)
+      for (int c = tid; c < a.cols >> 3; c += GROUP) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
+    return;
+  }
+  Logits8<E> v[NV];
+#pragma unroll
+  for (int j = 0; j < NV; j++) {
+    const int c = tid + j * GROUP;
+    v[j].none();
+    if (c < nvec) v[j].load(x + (int64_t)c * 8);
+  }
+  const float xt = tid == 0 && target < a.vocab ? (sizeof(E) == 2 ? __uint_as_float((uint32_t)((const bf16_t*)x)[target] << 16) : ((const float*)x)[target])
+                                                : __uint_as_float(0x7fc00000u);
+  if (tail)
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+      if (tid + j * GROUP == nvec - 1) v[j].keep(tail);
+  float m = largest<NV>(v), s = 0.f;
+  auto add = [&](const Logits8<E>& u, float m) {
+    float f[8];
+    u.get(f);
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f((f[e] - m) * LOG2E);
+    s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+  };
+  {
+    const float c = m == -INFINITY ? 0.f : m;          // nothing but -inf: s is 0 of no weight
+#pragma unroll
+    for (int j = 0; j < NV; j++) {
+      v[j].settle();
+      add(v[j], c);
     }
   }
+  for (int c = tid + NV * GROUP; c < nvec; c += GROUP) {
+    Logits8<E> u;
+    u.load(x + (int64_t)c * 8);
+    if (tail && c == nvec - 1) u.keep(tail);
+    const float n = fmaxf(m, largest<1>(&u));
+    if (n != m) {
+      s *= rescale(m, n);
+      m = n;
+    }
+    add(u, m == -INFINITY ? 0.f : m);
+  }
+  // all threads' (m, s) in one (without anything but -inf s ends as 0, and the differences of m below as NaN)
+  float top = m;
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
+  s = wave_sum(s * rescale(m, top));
+  if (WAVES > 1) {
+    if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = make_float2(top, s);
+    __syncthreads();
+    float2 w[WAVES];
+    float most = -INFINITY;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) { w[i] = wave_sums[i]; most = fmaxf(most, w[i].x); }
+    top = most;
+    s = 0.f;
+#pragma unroll
+    for (int i = 0; i < WAVES; i++) s += w[i].y * rescale(w[i].x, top);
+  }
+  if (tid == 0) a.loss[row] = (float)((double)log2f(s) * (1.0 / (double)LOG2E) + ((double)top - (double)xt));
+  if (!out) return;
+  const float weight = a.scale * (a.dloss ? a.dloss[row] : 1.f), size = fabsf(weight);
+  const uint32_t sign = weight < 0.f ? 0x80008000u : 0u;
+  const float shift = target < a.vocab ? log2f(size) - log2f(s) : __uint_as_float(0x7fc00000u);
+  auto put = [&](int c, const Logits8<E>& u) {
+    float f[8];
+    u.get(f);
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f(fmaf(f[e] - top, LOG2E, shift));
+    if (c == target >> 3)
+#pragma unroll
+      for (int e = 0; e < 8; e++) f[e] -= e == (target & 7) ? size : 0.f;
+    if (tail && c == nvec - 1)
+#pragma unroll
+      for (int e = 0; e < 8; e++) f[e] = e < tail ? f[e] : 0.f;
+    uint4 r = pack8(f);
+    r.x ^= sign; r.y ^= sign; r.z ^= sign; r.w ^= sign;
+    *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = r;
+  };
+#pragma unroll
+  for (int j = 0; j < NV; j++) {
+    v[j].settle();
+    if (tid + j * GROUP < nvec) put(tid + j * GROUP, v[j]);
+  }
+  for (int c = tid + NV * GROUP; c < nvec; c += GROUP) {
+    Logits8<E> u;
+    u.load(x + (int64_t)c * 8);
+    put(c, u);
+  }
+  for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
 }
 
 }  // namespace
@@ -624,11 +732,15 @@ hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamm
 hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   if (a.t == 0) return hipSuccess;
   ProfScope prof(PROF_ELEMENTWISE, (double)a.t * ((logits_fp32 ? 4.0 : 2.0) * (double)a.vocab + (a.dlogits ? 2.0 * (double)a.cols : 0.0)), s);
-  const dim3 grid((unsigned)std::min<int64_t>(a.t, MAX_GRID));
-  if (logits_fp32)
-    hipLaunchKernelGGL(xent_kernel<float>, grid, dim3(256), 0, s, a);
-  else
-    hipLaunchKernelGGL(xent_kernel<bf16_t>, grid, dim3(256), 0, s, a);
+  const int64_t nvec = ceil_div(a.vocab, 8), blocks = nvec <= 256 ? ceil_div(a.t, 4) : a.t;
+  const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
+#define CALL(E, GROUP, NV) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a)
+  if (logits_fp32) {
+    if (nvec <= 256) CALL(float, 64, 4); else if (nvec <= 2048) CALL(float, 256, 8); else if (nvec <= 4096) CALL(float, 1024, 4); else CALL(float, 1024, 8);
+  } else {
+    if (nvec <= 256) CALL(bf16_t, 64, 4); else if (nvec <= 2048) CALL(bf16_t, 256, 8); else if (nvec <= 8192) CALL(bf16_t, 1024, 8); else CALL(bf16_t, 1024, 16);
+  }
+#undef CALL
   return hipGetLastError();
 }
 
