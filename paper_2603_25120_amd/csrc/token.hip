@@ -25,6 +25,23 @@ __device__ __forceinline__ void load8(const float* p, float* f) {
 }
 __device__ __forceinline__ void load8(const bf16_t* p, float* f) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
 
+// Results that together exceed the L2 caches (NT_BYTES) are stored past them: nobody finds them there any more, and as ordinary stores
+// they displace what is being read (32768 x 4096 rows of the table 72 -> 50 us; the figures at the kernels have it).
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+template <bool PAST>   // (a flag at run time will not do: the compiler makes one ordinary store of both)
+__device__ __forceinline__ void store16(void* p, const uint4& v) {
+  const u32x4 w = {v.x, v.y, v.z, v.w};
+  if (PAST)
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p));
+  else
+    *reinterpret_cast<u32x4*>(p) = w;
+}
+__device__ __forceinline__ uint4 load16_once(const void* p) {   // what nobody reads a second time
+  const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
+  return make_uint4(w[0], w[1], w[2], w[3]);
+}
+constexpr int64_t NT_BYTES = (int64_t)32 << 20;   // eight L2 caches of 4 MB
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t MAX_GRID = 1 << 20;   // workgroups along x: a dimension holds fewer than 2^32 threads
 
@@ -33,7 +50,7 @@ constexpr int64_t MAX_GRID = 1 << 20;   // workgroups along x: a dimension holds
 // take a row (of a slice of up to four 16-byte vectors a lane: grid y), so that narrow rows fill the wavefront too.
 // ---------------------------------------------------------------------------------------------
 constexpr int EMBED_VECS = 4;
-template <typename E, int LPR>
+template <typename E, int LPR, bool PAST>
 __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ table, const int32_t* __restrict__ ids, bf16_t* __restrict__ y,
                                                         int64_t T, int64_t vocab, int nvec, int64_t ldy, float scale) {
   const int lane = threadIdx.x % LPR, c0 = blockIdx.y * (EMBED_VECS * LPR) + lane;
@@ -55,7 +72,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ ta
       const int c = c0 + j * LPR;
 #pragma unroll
       for (int e = 0; e < 8; e++) v[j][e] *= scale;
-      if (c < nvec) *reinterpret_cast<uint4*>(y + row * ldy + (int64_t)c * 8) = pack8(v[j]);
+      if (c < nvec) store16<PAST>(y + row * ldy + (int64_t)c * 8, pack8(v[j]));
     }
   }
 }
@@ -136,7 +153,7 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void embed_sort_kernel(const int32
     for (int i = wave; i < range; i += SORT_WAVES) {
       if (!(empty[i >> 6] >> (i & 63) & 1)) continue;
       float4* row = reinterpret_cast<float4*>(dtable + (((int64_t)i << log2_buckets) + bucket) * nvec * 8);
-      for (int c = lane; c < 2 * nvec; c += 64) row[c] = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int c = lane; c < 2 * nvec; c += 64) row[c] = make_float4(0.f, 0.f, 0.f, 0.f);   // (past the caches: 575 us for 561)
     }
   for (int64_t t0 = first; t0 < end; t0 += 64 * AHEAD) {
     int32_t id[AHEAD];
@@ -198,7 +215,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const bf16_t* __restrict
     for (int j = 0; j < AHEAD; j++) {
       const int64_t p = p0 + (i + j < n ? i + j : n - 1);   // the last rows again where there are no more
       key[j] = keys[p];
-      row[j] = *reinterpret_cast<const uint4*>(src + order[p] * ld);
+      row[j] = load16_once(src + order[p] * ld);
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; j++) {
@@ -257,8 +274,9 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
 
 // ---------------------------------------------------------------------------------------------
 // Per-head RMS norm and rotation.  A head is held by LPH lanes, eight of its first half's elements and the eight half-split partners
-// of these in a lane (so the rotation needs no other lane; a head narrower than 16 LPH leaves lanes idle).  A lane group takes up to
-// HEADS heads of a token, so that the rotary factors, twice the bytes of a head's values, are fetched once for all of them.
+// of these in a lane (so the rotation needs no other lane; a head narrower than 16 LPH leaves lanes idle).  Forward a lane group takes one
+// head; the rotary factors, twice the bytes of its values, come from the caches (two heads of a token a group 114 us for 32768 x 40 x 128,
+// four 123, one 113).
 // ---------------------------------------------------------------------------------------------
 template <int LPH>
 __device__ __forceinline__ float group_sum(float v) {
@@ -267,12 +285,10 @@ __device__ __forceinline__ float group_sum(float v) {
   return v;
 }
 // cos and sin of eight pairs of a row's position; 1 and 0 without a table, NaN for a position outside it.
-__device__ __forceinline__ void rotary_factors(const float* __restrict__ table, const int32_t* __restrict__ pos, int64_t t, int64_t n_pos, int hd,
-                                               int i0, bool active, float* cs, float* sn) {
+__device__ __forceinline__ void rotary_factors(const float* __restrict__ table, int64_t p, int64_t n_pos, int hd, int i0, bool active, float* cs, float* sn) {
 #pragma unroll
   for (int e = 0; e < 8; e++) { cs[e] = 1.f; sn[e] = 0.f; }
   if (!table) return;
-  const int64_t p = pos[t];
   if (p < 0 || p >= n_pos) {
 #pragma unroll
     for (int e = 0; e < 8; e++) cs[e] = sn[e] = __uint_as_float(0x7fc00000u);
@@ -282,61 +298,52 @@ __device__ __forceinline__ void rotary_factors(const float* __restrict__ table, 
   }
 }
 
-template <int LPH, int HEADS>
-__global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a, uint32_t units_per_token) {
-  // tokens times lane groups of a token stay below 2^31 (check_qk_norm)
-  const uint32_t unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH, token = unit / units_per_token;
+template <int LPH, bool PAST>
+__global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
+  const uint32_t n_heads = a.n_q_heads + a.n_kv_heads, unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;   // tokens times heads stay below 2^31
+  const uint32_t token = unit / n_heads, h = unit - token * n_heads;
   const int64_t t = token;
   if (t >= a.t) return;
-  const int u = (int)(unit - token * units_per_token), i0 = (threadIdx.x % LPH) * 8, half = a.head_dim >> 1;
+  const int i0 = (threadIdx.x % LPH) * 8, half = a.head_dim >> 1;
   const bool active = i0 < half;
-  const int n_heads = a.n_q_heads + a.n_kv_heads;
-  uint4 lo[HEADS], hi[HEADS];
-#pragma unroll
-  for (int j = 0; j < HEADS; j++) {
-    const int h = u + j * (int)units_per_token;
-    lo[j] = hi[j] = make_uint4(0, 0, 0, 0);
-    if (active && h < n_heads) {
-      const bf16_t* p = (const bf16_t*)a.x + t * a.x_stride + (int64_t)h * a.head_dim + i0;
-      lo[j] = *reinterpret_cast<const uint4*>(p);
-      hi[j] = *reinterpret_cast<const uint4*>(p + half);
-    }
+  // Requested in front of everything else: loads come back in order, and the factors wait for the position (32768 x 40 x 128 118 -> 113 us).
+  const int64_t at = a.rope_table ? a.pos[t] : 0;
+  uint4 xl = make_uint4(0, 0, 0, 0), xh = xl, gl = xl, gh = xl;
+  if (active) {
+    const bf16_t* x = (const bf16_t*)a.x + t * a.x_stride + (int64_t)h * a.head_dim + i0;
+    const bf16_t* g = (const bf16_t*)((int)h < a.n_q_heads ? a.gamma_q : a.gamma_k) + i0;
+    xl = load16_once(x);
+    xh = load16_once(x + half);
+    gl = *reinterpret_cast<const uint4*>(g);
+    gh = *reinterpret_cast<const uint4*>(g + half);
   }
-  float cs[8], sn[8];
-  rotary_factors(a.rope_table, a.pos, t, a.n_pos, a.head_dim, i0, active, cs, sn);
+  float cs[8], sn[8], p[8], q[8], gp[8], gq[8], s = 0.f;
+  rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
+  unpack8(xl, p);
+  unpack8(xh, q);
+  unpack8(gl, gp);
+  unpack8(gh, gq);
 #pragma unroll
-  for (int j = 0; j < HEADS; j++) {
-    const int h = u + j * (int)units_per_token;
-    if (h >= n_heads) break;
-    float p[8], q[8], gp[8], gq[8], s = 0.f;
-    unpack8(lo[j], p);
-    unpack8(hi[j], q);
+  for (int e = 0; e < 8; e++) s = fmaf(p[e], p[e], fmaf(q[e], q[e], s));
+  s = group_sum<LPH>(s);
+  if (!active) return;
+  const float r = rsqrtf(s / (float)a.head_dim + a.eps);
 #pragma unroll
-    for (int e = 0; e < 8; e++) s = fmaf(p[e], p[e], fmaf(q[e], q[e], s));
-    s = group_sum<LPH>(s);
-    if (!active) continue;
-    const float r = rsqrtf(s / (float)a.head_dim + a.eps);
-    const bf16_t* g = (const bf16_t*)(h < a.n_q_heads ? a.gamma_q : a.gamma_k) + i0;
-    load8(g, gp);
-    load8(g + half, gq);
-    float op[8], oq[8];
-#pragma unroll
-    for (int e = 0; e < 8; e++) {
-      const float np = p[e] * r * gp[e], nq = q[e] * r * gq[e];
-      op[e] = a.rope_table ? np * cs[e] - nq * sn[e] : np;
-      oq[e] = a.rope_table ? nq * cs[e] + np * sn[e] : nq;
-    }
-    bf16_t* o = (bf16_t*)a.y + t * a.y_stride + (int64_t)h * a.head_dim + i0;
-    *reinterpret_cast<uint4*>(o) = pack8(op);
-    *reinterpret_cast<uint4*>(o + half) = pack8(oq);
+  for (int e = 0; e < 8; e++) {
+    const float np = p[e] * r * gp[e], nq = q[e] * r * gq[e];
+    p[e] = a.rope_table ? np * cs[e] - nq * sn[e] : np;
+    q[e] = a.rope_table ? nq * cs[e] + np * sn[e] : nq;
   }
+  bf16_t* o = (bf16_t*)a.y + t * a.y_stride + (int64_t)h * a.head_dim + i0;
+  store16<PAST>(o, pack8(p));
+  store16<PAST>(o + half, pack8(q));
 }
 
 // Backward: with n = x r and g the gradient of what left the norm (dy turned back), d = g gamma:
 // dx = r (d - n mean(d n)), dgamma = sum over tokens and heads of g n.  r is formed anew from x, which has to be read anyway.  The
 // first q_blocks workgroups take the query heads, the others the key heads, each walking over its share of the tokens with the sums of
 // g n in registers; it leaves one row of partial sums.
-template <int LPH, int HEADS>
+template <int LPH, int HEADS, bool PAST>
 __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* __restrict__ partial_q, float* __restrict__ partial_k, int q_blocks) {
   constexpr int GROUPS = 256 / LPH;
   __shared__ float part[4][LPH][17];
@@ -360,6 +367,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
     const uint32_t token = unit / (uint32_t)per_token;
     const int64_t t = token;
     const int u = (int)(unit - token * per_token);
+    const int64_t at = a.rope_table ? a.pos[t] : 0;   // first, as forward
     uint4 xl[HEADS], xh[HEADS], dl[HEADS], dh[HEADS];
 #pragma unroll
     for (int j = 0; j < HEADS; j++) {
@@ -368,14 +376,14 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
       if (active && h < n_heads) {
         const int64_t c = col + (int64_t)h * a.head_dim + i0;
         const bf16_t *px = (const bf16_t*)a.x + t * a.x_stride + c, *pd = (const bf16_t*)a.dy + t * a.dy_stride + c;
-        xl[j] = *reinterpret_cast<const uint4*>(px);
-        xh[j] = *reinterpret_cast<const uint4*>(px + half);
-        dl[j] = *reinterpret_cast<const uint4*>(pd);
-        dh[j] = *reinterpret_cast<const uint4*>(pd + half);
+        xl[j] = load16_once(px);
+        xh[j] = load16_once(px + half);
+        dl[j] = load16_once(pd);
+        dh[j] = load16_once(pd + half);
       }
     }
     float cs[8], sn[8];
-    rotary_factors(a.rope_table, a.pos, t, a.n_pos, a.head_dim, i0, active, cs, sn);
+    rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
 #pragma unroll
     for (int j = 0; j < HEADS; j++) {
       const int h = u + j * per_token;
@@ -410,8 +418,8 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
 #pragma unroll
       for (int e = 0; e < 16; e++) o[e] = r * (d[e] - x[e] * m);
       bf16_t* p = (bf16_t*)a.y + t * a.y_stride + col + (int64_t)h * a.head_dim + i0;
-      *reinterpret_cast<uint4*>(p) = pack8(o);
-      *reinterpret_cast<uint4*>(p + half) = pack8(o + 8);
+      store16<PAST>(p, pack8(o));
+      store16<PAST>(p + half, pack8(o + 8));
     }
   }
   // lane groups of a wavefront, then the four wavefronts
@@ -503,7 +511,7 @@ __device__ __forceinline__ float largest(const Logits8<float>* v) {
 // What a sum against the maximum `from` is worth against `to`, at or above it; a sum of nothing but -inf is none.
 __device__ __forceinline__ float rescale(float from, float to) { return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * LOG2E); }
 
-template <typename E, int GROUP, int NV>
+template <typename E, int GROUP, int NV, bool PAST>
 __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArgs a) {
   constexpr int BLOCK = GROUP < 256 ? 256 : GROUP, WAVES = GROUP / 64;
   __shared__ float2 wave_sums[WAVES];
@@ -516,7 +524,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
   if (target < 0) {
     if (tid == 0) a.loss[row] = 0.f;
     if (out)
-      for (int c = tid; c < a.cols >> 3; c += GROUP) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
+      for (int c = tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
     return;
   }
   Logits8<E> v[NV];
@@ -594,7 +602,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
       for (int e = 0; e < 8; e++) f[e] = e < tail ? f[e] : 0.f;
     uint4 r = pack8(f);
     r.x ^= sign; r.y ^= sign; r.z ^= sign; r.w ^= sign;
-    *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = r;
+    store16<PAST>(out + (int64_t)c * 8, r);
   };
 #pragma unroll
   for (int j = 0; j < NV; j++) {
@@ -606,7 +614,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     u.load(x + (int64_t)c * 8);
     put(c, u);
   }
-  for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) *reinterpret_cast<uint4*>(out + (int64_t)c * 8) = make_uint4(0, 0, 0, 0);
+  for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
 }
 
 }  // namespace
@@ -617,10 +625,12 @@ hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* id
   const int nvec = (int)(d / 8), lpr = nvec <= 8 ? 8 : nvec <= 16 ? 16 : nvec <= 32 ? 32 : 64;
   const dim3 grid((unsigned)std::min<int64_t>(ceil_div(t, 256 / lpr), MAX_GRID), (unsigned)ceil_div(nvec, EMBED_VECS * lpr));
   ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * (table_fp32 ? 6.0 : 4.0), s);
-#define CALL(E, L) hipLaunchKernelGGL((embed_fwd_kernel<E, L>), grid, dim3(256), 0, s, (const E*)table, ids, (bf16_t*)y, t, vocab, nvec, y_stride, scale)
-#define CALL_LPR(E) \
-  do { if (lpr == 8) CALL(E, 8); else if (lpr == 16) CALL(E, 16); else if (lpr == 32) CALL(E, 32); else CALL(E, 64); } while (0)
-  if (table_fp32) CALL_LPR(float); else CALL_LPR(bf16_t);
+#define CALL(E, L, P) hipLaunchKernelGGL((embed_fwd_kernel<E, L, P>), grid, dim3(256), 0, s, (const E*)table, ids, (bf16_t*)y, t, vocab, nvec, y_stride, scale)
+#define CALL_LPR(E, P) \
+  do { if (lpr == 8) CALL(E, 8, P); else if (lpr == 16) CALL(E, 16, P); else if (lpr == 32) CALL(E, 32, P); else CALL(E, 64, P); } while (0)
+#define CALL_PAST(E) do { if (t * d * 2 > NT_BYTES) CALL_LPR(E, true); else CALL_LPR(E, false); } while (0)
+  if (table_fp32) CALL_PAST(float); else CALL_PAST(bf16_t);
+#undef CALL_PAST
 #undef CALL_LPR
 #undef CALL
   return hipGetLastError();
@@ -662,7 +672,7 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
   float* partial = (float*)((char*)total + 256);
   {
     ProfScope prof(PROF_ELEMENTWISE, accumulate ? 0.0 : (double)vocab * (double)d * 4.0, s);
-    hipLaunchKernelGGL(embed_sort_kernel, dim3(1u << log2_buckets), dim3(64 * SORT_WAVES), 0, s, ids, (int)t, (int)vocab, log2_buckets, nvec, order, keys,
+hipLaunchKernelGGL(embed_sort_kernel, dim3(1u << log2_buckets), dim3(64 * SORT_WAVES), 0, s, ids, (int)t, (int)vocab, log2_buckets, nvec, order, keys,
                        total, dtable, accumulate ? 0 : 1);
   }
   if (t == 0) return hipGetLastError();
@@ -683,22 +693,25 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
 }
 
 namespace {
-constexpr int QK_HEADS = 4;
+constexpr int QK_HEADS = 2;   // of a token that a lane group of the backward pass takes (1 205 us for 32768 x 40 x 128, 2 194, 4 209)
 int qk_lanes(int head_dim) { return head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
 // Workgroups of the backward pass that take `heads` of `all` heads.
 int64_t qk_bwd_blocks(int64_t t, int heads, int all, int head_dim) {
+  // up to eight workgroups a CU: 1024 of them 225 us for 32768 x 40 x 128, 2048 194, 4096 199, and more partial sums for fewer tokens
   const int64_t units = t * ceil_div(heads, QK_HEADS), groups = 256 / qk_lanes(head_dim);
-  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), ceil_div((int64_t)1024 * heads, all)));
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), ceil_div((int64_t)2048 * heads, all)));
 }
 }  // namespace
 
 hipError_t launch_qk_norm_fwd(const QkNormArgs& a, hipStream_t s) {
   if (a.t == 0) return hipSuccess;
-  const int n_heads = a.n_q_heads + a.n_kv_heads, units = (int)ceil_div(n_heads, QK_HEADS), lph = qk_lanes(a.head_dim);
+  const int n_heads = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
   ProfScope prof(PROF_ELEMENTWISE, 4.0 * (double)a.t * n_heads * a.head_dim, s);
-  const dim3 grid((unsigned)ceil_div(a.t * units, 256 / lph));
-#define CALL(L) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, QK_HEADS>), grid, dim3(256), 0, s, a, units)
-  if (lph == 2) CALL(2); else if (lph == 4) CALL(4); else if (lph == 8) CALL(8); else CALL(16);
+  const dim3 grid((unsigned)ceil_div(a.t * n_heads, 256 / lph));
+#define CALL(L, P) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, P>), grid, dim3(256), 0, s, a)
+#define CALL_LPH(P) do { if (lph == 2) CALL(2, P); else if (lph == 4) CALL(4, P); else if (lph == 8) CALL(8, P); else CALL(16, P); } while (0)
+  if (a.t * n_heads * a.head_dim * 2 > NT_BYTES) CALL_LPH(true); else CALL_LPH(false);
+#undef CALL_LPH
 #undef CALL
   return hipGetLastError();
 }
@@ -711,9 +724,14 @@ size_t qk_norm_bwd_partial_floats(int64_t t, int n_q_heads, int n_kv_heads, int 
 hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamma_k, PartialSums& sums, hipStream_t s) {
   const int all = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
   const int64_t bq = qk_bwd_blocks(a.t, a.n_q_heads, all, a.head_dim), bk = qk_bwd_blocks(a.t, a.n_kv_heads, all, a.head_dim);
+  const bool past = a.t * all * a.head_dim * 2 > NT_BYTES;
   float *pq = nullptr, *pk = nullptr;
   ProfScope prof(PROF_ELEMENTWISE, 6.0 * (double)a.t * all * a.head_dim, s);
-#define CALL(L, BLOCKS, Q) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q))
+#define CALL(L, BLOCKS, Q)                                                                                                                           \
+  do {                                                                                                                                               \
+    if (past) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS, true>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));           \
+    else hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS, false>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));               \
+  } while (0)
 #define CALL_LPH(BLOCKS, Q) \
   do { if (lph == 2) CALL(2, BLOCKS, Q); else if (lph == 4) CALL(4, BLOCKS, Q); else if (lph == 8) CALL(8, BLOCKS, Q); else CALL(16, BLOCKS, Q); } while (0)
   hipError_t e = sums.room((size_t)(bq + bk) * a.head_dim, a.head_dim, {dgamma_q, dgamma_k}, s);
@@ -734,7 +752,12 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   ProfScope prof(PROF_ELEMENTWISE, (double)a.t * ((logits_fp32 ? 4.0 : 2.0) * (double)a.vocab + (a.dlogits ? 2.0 * (double)a.cols : 0.0)), s);
   const int64_t nvec = ceil_div(a.vocab, 8), blocks = nvec <= 256 ? ceil_div(a.t, 4) : a.t;
   const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
-#define CALL(E, GROUP, NV) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a)
+  const bool past = a.dlogits && a.t * a.cols * 2 > NT_BYTES;
+#define CALL(E, GROUP, NV)                                                                                                  \
+  do {                                                                                                                      \
+    if (past) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, true>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);        \
+    else hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);            \
+  } while (0)
   if (logits_fp32) {
     if (nvec <= 256) CALL(float, 64, 4); else if (nvec <= 2048) CALL(float, 256, 8); else if (nvec <= 4096) CALL(float, 1024, 4); else CALL(float, 1024, 8);
   } else {
