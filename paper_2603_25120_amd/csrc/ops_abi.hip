@@ -507,8 +507,8 @@ static mllm_status_t check_qk_norm(const QkNormArgs& a) {
   if (a.n_q_heads <= 0 || a.n_kv_heads <= 0 || a.n_q_heads > 65536 || a.n_kv_heads > 65536)
     return op_fail(MLLM_ERR_SHAPE, "n_q_heads and n_kv_heads must be positive, at most 65536");
   const int64_t heads = (int64_t)a.n_q_heads + a.n_kv_heads, width = heads * a.head_dim;
-  if (a.t < 0 || a.t * heads > MAX_ROWS) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, t times the heads below 2^31");
-  if (a.t * width * 2 > ((int64_t)1 << 40)) return op_fail(MLLM_ERR_SHAPE, "more than 2^40 bytes of heads");   // a launch's grid
+  // a lane group of up to 16 a head, and fewer than 2^32 threads in a launch
+  if (a.t < 0 || a.t > MAX_ROWS || a.t * heads >= ((int64_t)1 << 28)) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, t times the heads below 2^28");
   if (!(a.eps >= 0.f)) return op_fail(MLLM_ERR_SHAPE, "eps must not be negative");
   if (a.rope_table && a.n_pos < 0) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative");
   CHECK(check_rows("x", a.x, width, a.x_stride));
@@ -557,7 +557,10 @@ mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* t
   CHECK(check_rows("logits", logits, cols, logits_stride));
   if (dlogits) {
     CHECK(check_rows("dlogits", dlogits, cols, dlogits_stride));
-    const int64_t in = ((t - 1) * logits_stride + cols) * (logits_fp32 ? 4 : 2), out = ((t - 1) * dlogits_stride + cols) * 2;
+    const auto span = [&](int64_t stride, int bytes) {
+      return (int64_t)std::min<__int128>(((__int128)(t - 1) * stride + cols) * bytes, INT64_MAX / 4);
+    };
+    const int64_t in = span(logits_stride, logits_fp32 ? 4 : 2), out = span(dlogits_stride, 2);
     if (t > 0 && ranges_overlap(logits, in, dlogits, out) && (dlogits != logits || logits_fp32 || dlogits_stride != logits_stride))
       return op_fail(MLLM_ERR_UNSUPPORTED, "dlogits may be logits (bf16, same stride) but not overlap them otherwise");
   }

@@ -300,7 +300,7 @@ __device__ __forceinline__ void rotary_factors(const float* __restrict__ table, 
 
 template <int LPH, bool PAST>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
-  const uint32_t n_heads = a.n_q_heads + a.n_kv_heads, unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;   // tokens times heads stay below 2^31
+  const uint32_t n_heads = a.n_q_heads + a.n_kv_heads, unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;   // tokens times heads stay below 2^28
   const uint32_t token = unit / n_heads, h = unit - token * n_heads;
   const int64_t t = token;
   if (t >= a.t) return;
@@ -362,7 +362,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
     load8(gamma + half, g + 8);
   }
   const float inv = 1.f / (float)a.head_dim;
-  const uint32_t units = (uint32_t)a.t * per_token;   // below 2^31, as forward
+  const uint32_t units = (uint32_t)a.t * per_token;   // below 2^28, as forward
   for (uint32_t unit = block * GROUPS + threadIdx.x / LPH; unit < units; unit += blocks * GROUPS) {
     const uint32_t token = unit / (uint32_t)per_token;
     const int64_t t = token;
