@@ -244,18 +244,22 @@ def attention_bwd(do, q, k, v, cu, mask_kind):
 # QK normalisation (layer variant of the evaluated encoders, Evaluation, Table 4: InternViT).  The
 # query row of a token (all its heads side by side) and its key row each pass through an RMSNorm
 # with a gain vector of their own; in a decoder layer this comes before the rotary embedding.
+# qk_norm = 3: every head is a row of its own, the heads share a gain vector of head_dim values.
 # ---------------------------------------------------------------------------
+def _norm_rows(z, g):
+    """[T, H, hd] as the rows that a gain of this width normalises."""
+    return z.reshape(-1, np.size(g))
+
+
 def qk_norm_fwd(q, k, gq, gk, eps):
-    T = q.shape[0]
-    qn, cq = rmsnorm_fwd(q.reshape(T, -1), gq, eps)
-    kn, ck = rmsnorm_fwd(k.reshape(T, -1), gk, eps)
+    qn, cq = rmsnorm_fwd(_norm_rows(q, gq), gq, eps)
+    kn, ck = rmsnorm_fwd(_norm_rows(k, gk), gk, eps)
     return qn.reshape(q.shape), kn.reshape(k.shape), cq, ck
 
 
 def qk_norm_bwd(dq, dk, cq, ck, gq, gk):
-    T = dq.shape[0]
-    dqp, d_gq = rmsnorm_bwd(dq.reshape(T, -1), cq, gq)
-    dkp, d_gk = rmsnorm_bwd(dk.reshape(T, -1), ck, gk)
+    dqp, d_gq = rmsnorm_bwd(_norm_rows(dq, gq), cq, gq)
+    dkp, d_gk = rmsnorm_bwd(_norm_rows(dk, gk), ck, gk)
     return dqp.reshape(dq.shape), dkp.reshape(dk.shape), d_gq, d_gk
 
 

@@ -51,6 +51,7 @@ struct ParamInfo {
   int64_t rows, cols;
 };
 
+bool per_head(const mllm_layer_desc_t& L) { return L.qk_norm & MLLM_QK_NORM_PER_HEAD; }
 int64_t nqkv_of(const mllm_layer_desc_t& L) { return (int64_t)(L.n_q_heads + 2 * L.n_kv_heads) * L.head_dim; }
 
 }  // namespace
@@ -97,7 +98,8 @@ mllm_status_t check_layer(const mllm_layer_desc_t& L, int i) {
   if (!m64(L.d_model) || !m64(L.d_ff)) return fail(MLLM_ERR_DESC, "layer %d: widths must be positive multiples of 64", i);
   if (L.d_model > 8192) return fail(MLLM_ERR_DESC, "layer %d: d_model above 8192", i);
   if (!(L.norm_eps > 0.f)) return fail(MLLM_ERR_DESC, "layer %d: norm_eps must be positive", i);
-  if (L.qk_norm != 0 && L.qk_norm != 1) return fail(MLLM_ERR_DESC, "layer %d: qk_norm must be 0 or 1", i);
+  if (L.qk_norm != 0 && L.qk_norm != MLLM_QK_NORM && L.qk_norm != (MLLM_QK_NORM | MLLM_QK_NORM_PER_HEAD))
+    return fail(MLLM_ERR_DESC, "layer %d: qk_norm must be 0, MLLM_QK_NORM or MLLM_QK_NORM | MLLM_QK_NORM_PER_HEAD", i);
   if (L.kind == MLLM_LAYER_VIT) {
     if (L.has_bias != 1) return fail(MLLM_ERR_DESC, "layer %d: ViT layer needs has_bias = 1", i);
     if (L.act != MLLM_ACT_GELU_ERF && L.act != MLLM_ACT_GELU_TANH) return fail(MLLM_ERR_DESC, "layer %d: ViT activation must be GELU", i);
@@ -182,7 +184,8 @@ struct Bump {
 struct LayerSaved {  // byte offsets into `saved`
   size_t x, stats1, n1, qkv, o, lse, x1, stats2, n2, pre, act;
   // QK normalisation only: qkv then keeps the projection's q and k, and qkn [T, nq] holds the
-  // normalised (and rotated) q and k in the same columns (its v columns are unused)
+  // normalised (and rotated) q and k in the same columns (its v columns are unused).  Per-head norms keep no statistics:
+  // a head is read anyway
   size_t qkn, statsq, statsk;
 };
 
@@ -250,7 +253,9 @@ size_t layer_partial_bytes(const mllm_layer_desc_t& L, int64_t T) {
   int64_t floats = 2 * norm_bwd_workgroups(T, d) * d * norm_bwd_sets(vit ? 0 : 1, fused);
   if (vit) floats += colsum_partial_rows(T) * (d + (fused ? 0 : d) + L.d_ff);
   if (vit || L.has_bias) floats += colsum_partial_rows(T) * nqkv_of(L);
-  if (L.qk_norm)   // these two have no room of their own (they flush what waits when it is full), but each fits alone
+  if (per_head(L))   // one take (both gains together)
+    floats = std::max(floats, (int64_t)qk_norm_bwd_partial_floats(T, L.n_q_heads, L.n_kv_heads, L.head_dim));
+  else if (L.qk_norm)   // these two have no room of their own (they flush what waits when it is full), but each fits alone
     for (int64_t w : {(int64_t)L.n_q_heads * L.head_dim, (int64_t)L.n_kv_heads * L.head_dim}) floats = std::max(floats, norm_bwd_workgroups(T, w) * w);
   return (size_t)floats * 4;
 }
@@ -312,8 +317,10 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
     S.qkv = sv.take(T * nqkv_of(L) * 2);
     if (L.qk_norm) {
       S.qkn = sv.take(T * nqkv_of(L) * 2);
-      S.statsq = sv.take(T * 2 * 4);
-      S.statsk = sv.take(T * 2 * 4);
+      if (!per_head(L)) {
+        S.statsq = sv.take(T * 2 * 4);
+        S.statsk = sv.take(T * 2 * 4);
+      }
     }
     S.o = sv.take(T * d * 2);
     S.lse = sv.take(T * L.n_q_heads * 4);
@@ -594,6 +601,13 @@ AttnArgs attn_args(const mllm_layer_desc_t& L, char* qk, char* v, int64_t T, con
   return a;
 }
 
+// Per-head QK normalisation of the [T, nq] matrix x, to y or (dy the gradient of the normalised heads) its gradient to y.
+QkNormArgs qk_norm_args(const mllm_layer_desc_t& L, const void* const* gains, const void* x, const void* dy, void* y, int64_t T, const float* rope_table,
+                        const int32_t* pos, int64_t n_pos) {
+  const int64_t nq = nqkv_of(L);
+  return {x, dy, y, gains[0], gains[1], pos, rope_table, n_pos, T, nq, nq, nq, L.n_q_heads, L.n_kv_heads, L.head_dim, L.norm_eps};
+}
+
 #define K_TRY(expr)                                                                        \
   do {                                                                                     \
     hipError_t e_ = (expr);                                                                \
@@ -640,13 +654,17 @@ mllm_status_t layer_fwd(const mllm_layer_desc_t& L, const void* const* prm, cons
   else
     K_TRY(linear_fwd(n1, wqkv, qkv, T, d, nq, bqkv, nullptr, s, split));
   char* qk = qkv;
-  if (L.qk_norm) {
+  if (per_head(L)) {   // rotation and all
+    qk = saved + S.qkn;
+    K_TRY(launch_qk_norm_fwd(qk_norm_args(L, prm + n_base, qkv, nullptr, qk, T, vit ? nullptr : rope_table, (const int32_t*)(ws + P.meta.pos),
+                                          P.longest_seq), s));
+  } else if (L.qk_norm) {
     qk = saved + S.qkn;
     K_TRY(launch_norm_fwd(1, qkv, prm[n_base], nullptr, qk, (float*)(saved + S.statsq), T, q_cols, nq, L.norm_eps, s));
     K_TRY(launch_norm_fwd(1, qkv + q_cols * 2, prm[n_base + 1], nullptr, qk + q_cols * 2,
                           (float*)(saved + S.statsk), T, k_cols, nq, L.norm_eps, s));
   }
-  if (!vit && !rope_fused)
+  if (!vit && !rope_fused && !per_head(L))
     K_TRY(launch_rope_from_table(qk, (const int32_t*)(ws + P.meta.pos), rope_table, T, nq, L.n_q_heads + L.n_kv_heads,
                                  L.head_dim, s));
   AttnArgs a = attn_args(L, qk, qkv, T, ws, P, vit, attn_list);
@@ -733,7 +751,9 @@ mllm_status_t layer_bwd(const mllm_layer_desc_t& L, const void* const* prm, void
   a.delta = (float*)(ws + P.w_delta);
   a.rope_table = vit ? nullptr : rope_table;   // dq, dk leave the kernels rotated back (the rotation's gradient)
   K_TRY(launch_attn_bwd(a, s));
-  if (L.qk_norm) {
+  if (per_head(L)) {
+    K_TRY(launch_qk_norm_bwd(qk_norm_args(L, prm + n_base, qkv, dqk, we, T, nullptr, nullptr, 0), (float*)dprm[n_base], (float*)dprm[n_base + 1], sums, s));
+  } else if (L.qk_norm) {
     K_TRY(launch_norm_bwd(1, dqk, qkv, prm[n_base], (const float*)(saved + S.statsq), nullptr, we,
                           (float*)dprm[n_base], nullptr, sums, T, q_cols, nq, s));
     K_TRY(launch_norm_bwd(1, dqk + q_cols * 2, qkv + q_cols * 2, prm[n_base + 1], (const float*)(saved + S.statsk),
@@ -828,8 +848,8 @@ mllm_status_t mllm_stage_create(const mllm_stage_desc_t* desc, mllm_stage_t** ou
       st->params.insert(st->params.end(), std::begin(ps), std::end(ps));
     }
     if (L.kind != MLLM_LAYER_PROJECTOR && L.qk_norm) {
-      st->params.push_back({"qkn_q_g", i, 1, (int64_t)L.n_q_heads * L.head_dim});
-      st->params.push_back({"qkn_k_g", i, 1, (int64_t)L.n_kv_heads * L.head_dim});
+      st->params.push_back({"qkn_q_g", i, 1, (int64_t)(per_head(L) ? 1 : L.n_q_heads) * L.head_dim});
+      st->params.push_back({"qkn_k_g", i, 1, (int64_t)(per_head(L) ? 1 : L.n_kv_heads) * L.head_dim});
     }
   }
   *out = st;

@@ -27,6 +27,7 @@ import numpy as np
 LAYER_VIT, LAYER_DECODER, LAYER_PROJECTOR = 0, 1, 2
 ACT_GELU_ERF, ACT_GELU_TANH, ACT_SWIGLU = 0, 1, 2
 MASK_BIDIR, MASK_CAUSAL = 0, 1
+QK_NORM_HEADS = 3       # MLLM_QK_NORM | MLLM_QK_NORM_PER_HEAD
 
 IMG_TOKENS = 576  # 24 x 24 patches of a 336-pixel image at patch size 14
 
@@ -69,12 +70,13 @@ class LayerDesc:
     rope_base: float = 10000.0
     pool: int = 0           # projector: average-pool this many consecutive encoder tokens first (0/1: none)
     merge: int = 0          # projector: concatenate this many consecutive encoder tokens into one row (0/1: none)
-    qk_norm: int = 0        # ViT / decoder: RMS-normalise the q rows and the k rows (all heads together) before attention
+    qk_norm: int = 0        # ViT / decoder: RMS-normalise the q rows and the k rows (all heads together; 3: every head) before attention
 
 
 def vit_layer(d, heads, head_dim, d_ff, eps=1e-5, act=ACT_GELU_ERF, qk_norm=0) -> LayerDesc:
     """qk_norm = 1: the query rows and the key rows (all heads of a token together) pass through an
-    RMSNorm with a gain of their own before attention (the InternViT kind of QK normalisation)."""
+    RMSNorm with a gain of their own before attention (the InternViT kind of QK normalisation);
+    QK_NORM_HEADS: every head on its own, with gains that the heads share."""
     return LayerDesc(LAYER_VIT, d, heads, heads, head_dim, d_ff, 0, act, 1, eps, 0.0, qk_norm=qk_norm)
 
 
@@ -95,6 +97,12 @@ def projector_layer(d_in, d_out, d_hidden=0, act=ACT_GELU_ERF, pool=0, merge=0) 
     return LayerDesc(LAYER_PROJECTOR, d_in, 0, 0, 0, d_hidden, d_out, act if d_hidden else 0, 1, 0.0, 0.0, pool, merge)
 
 
+def qk_gains(layer: LayerDesc) -> List[Tuple[str, int, int]]:
+    """The gains of QK normalisation: of the whole rows, or (qk_norm = 3) of a head, shared by all."""
+    hq, hkv = (1, 1) if layer.qk_norm == QK_NORM_HEADS else (layer.n_q_heads, layer.n_kv_heads)
+    return [("qkn_q_g", 1, hq * layer.head_dim), ("qkn_k_g", 1, hkv * layer.head_dim)] if layer.qk_norm else []
+
+
 def param_specs(layer: LayerDesc) -> List[Tuple[str, int, int]]:
     """(name, rows, cols) of every parameter tensor of a layer, in interface order.
 
@@ -106,7 +114,7 @@ def param_specs(layer: LayerDesc) -> List[Tuple[str, int, int]]:
         nqkv = (layer.n_q_heads + 2 * layer.n_kv_heads) * layer.head_dim
         no = layer.n_q_heads * layer.head_dim
         f = layer.d_ff
-        qkn = [("qkn_q_g", 1, no), ("qkn_k_g", 1, layer.n_kv_heads * layer.head_dim)] if layer.qk_norm else []
+        qkn = qk_gains(layer)
         return [("ln1_g", 1, d), ("ln1_b", 1, d), ("w_qkv", d, nqkv), ("b_qkv", 1, nqkv),
                 ("w_o", no, d), ("b_o", 1, d), ("ln2_g", 1, d), ("ln2_b", 1, d),
                 ("w_1", d, f), ("b_1", 1, f), ("w_2", f, d), ("b_2", 1, d)] + qkn
@@ -115,7 +123,7 @@ def param_specs(layer: LayerDesc) -> List[Tuple[str, int, int]]:
         no = layer.n_q_heads * layer.head_dim
         f = layer.d_ff
         qkv = [("w_qkv", d, nqkv), ("b_qkv", 1, nqkv)] if layer.has_bias else [("w_qkv", d, nqkv)]
-        qkn = [("qkn_q_g", 1, no), ("qkn_k_g", 1, layer.n_kv_heads * layer.head_dim)] if layer.qk_norm else []
+        qkn = qk_gains(layer)
         return [("rms1_g", 1, d)] + qkv + [("w_o", no, d), ("rms2_g", 1, d), ("w_gu", d, 2 * f), ("w_d", f, d)] + qkn
     if layer.kind == LAYER_PROJECTOR:
         d_in = d * max(1, layer.merge)
@@ -336,6 +344,18 @@ def workload_tiny_qknorm(seed: int) -> Workload:
     samples = [(1, int(rng.integers(32, 97))) for _ in range(2)]
     batch = batch_from_samples(samples, img_tokens=64)
     return make_workload("tiny_qknorm", tiny_qknorm_layers(), batch, seed)
+
+
+def tiny_headnorm_layers() -> List[LayerDesc]:
+    """The tiny stage with every query and key head normalised on its own: an encoder layer and two grouped-query decoder layers."""
+    dec = decoder_layer(256, 4, 2, 64, 1024, 10000.0, qk_norm=QK_NORM_HEADS)
+    return [vit_layer(192, 3, 64, 768, qk_norm=QK_NORM_HEADS), projector_layer(192, 256), dec, dec]
+
+
+def workload_tiny_headnorm(seed: int) -> Workload:
+    rng = np.random.default_rng(seed)
+    samples = [(1, int(rng.integers(32, 97))) for _ in range(2)]
+    return make_workload("tiny_headnorm", tiny_headnorm_layers(), batch_from_samples(samples, img_tokens=64), seed)
 
 
 def tiny_pooled_layers() -> List[LayerDesc]:
