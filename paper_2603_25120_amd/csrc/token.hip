@@ -42,6 +42,28 @@ __device__ __forceinline__ uint4 load16_once(const void* p) {   // what nobody r
 }
 constexpr int64_t NT_BYTES = (int64_t)32 << 20;   // eight L2 caches of 4 MB
 
+// What 2, 4, 8, 16 or 64 neighbouring lanes hold, added up or the largest, in all of them: exchanges inside the vector unit (through LDS, as
+// __shfl_xor goes, a step is some fifty cycles).
+template <int CTRL>
+__device__ __forceinline__ float from_lane(float v) { return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true)); }
+template <bool MAX>
+__device__ __forceinline__ float joined(float a, float b) { return MAX ? fmaxf(a, b) : a + b; }
+template <int LANES, bool MAX>
+__device__ __forceinline__ float over_lanes(float v) {
+  static_assert(LANES == 2 || LANES == 4 || LANES == 8 || LANES == 16 || LANES == 64, "whole groups of lanes");
+  v = joined<MAX>(v, from_lane<0xb1>(v));                       // the other one of a pair
+  if (LANES > 2) v = joined<MAX>(v, from_lane<0x4e>(v));        // the other pair of four
+  if (LANES > 4) v = joined<MAX>(v, from_lane<0x141>(v));       // a row's halves mirrored: the other four
+  if (LANES > 8) v = joined<MAX>(v, from_lane<0x140>(v));       // a row mirrored: the other eight
+  if (LANES > 16) {
+    auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = joined<MAX>(__uint_as_float(w[0]), __uint_as_float(w[1]));
+    w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+    v = joined<MAX>(__uint_as_float(w[0]), __uint_as_float(w[1]));
+  }
+  return v;
+}
+
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t MAX_GRID = 1 << 20;   // workgroups along x: a dimension holds fewer than 2^32 threads
 
@@ -325,27 +347,17 @@ __global__ __launch_bounds__(256) void embed_join_kernel(const int32_t* __restri
 // head; the rotary factors, twice the bytes of its values, come from the caches (two heads of a token a group 114 us for 32768 x 40 x 128,
 // four 123, one 113).
 // ---------------------------------------------------------------------------------------------
-template <int LPH>
-__device__ __forceinline__ float group_sum(float v) {
-#pragma unroll
-  for (int o = LPH / 2; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
-// cos and sin of eight pairs of a row's position; 1 and 0 without a table, NaN for a position outside it.
+// cos and sin of eight pairs of a row's position, NaN for a position outside the table (0 in lanes that hold nothing).
 __device__ __forceinline__ void rotary_factors(const float* __restrict__ table, int64_t p, int64_t n_pos, int hd, int i0, bool active, float* cs, float* sn) {
 #pragma unroll
-  for (int e = 0; e < 8; e++) { cs[e] = 1.f; sn[e] = 0.f; }
-  if (!table) return;
-  if (p < 0 || p >= n_pos) {
-#pragma unroll
-    for (int e = 0; e < 8; e++) cs[e] = sn[e] = __uint_as_float(0x7fc00000u);
-  } else if (active) {
+  for (int e = 0; e < 8; e++) cs[e] = sn[e] = active ? __uint_as_float(0x7fc00000u) : 0.f;
+  if (active && p >= 0 && p < n_pos) {
     load8(table + p * hd + i0, cs);
     load8(table + p * hd + hd / 2 + i0, sn);
   }
 }
 
-template <int LPH, bool PAST>
+template <int LPH, bool ROTATE, bool PAST>
 __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
   const uint32_t n_heads = a.n_q_heads + a.n_kv_heads, unit = blockIdx.x * (256 / LPH) + threadIdx.x / LPH;   // tokens times heads stay below 2^28
   const uint32_t token = unit / n_heads, h = unit - token * n_heads;
@@ -354,7 +366,7 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
   const int i0 = (threadIdx.x % LPH) * 8, half = a.head_dim >> 1;
   const bool active = i0 < half;
   // Requested in front of everything else: loads come back in order, and the factors wait for the position (32768 x 40 x 128 118 -> 113 us).
-  const int64_t at = a.rope_table ? a.pos[t] : 0;
+  const int64_t at = ROTATE ? a.pos[t] : 0;
   uint4 xl = make_uint4(0, 0, 0, 0), xh = xl, gl = xl, gh = xl;
   if (active) {
     const bf16_t* x = (const bf16_t*)a.x + t * a.x_stride + (int64_t)h * a.head_dim + i0;
@@ -365,21 +377,21 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
     gh = *reinterpret_cast<const uint4*>(g + half);
   }
   float cs[8], sn[8], p[8], q[8], gp[8], gq[8], s = 0.f;
-  rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
+  if (ROTATE) rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
   unpack8(xl, p);
   unpack8(xh, q);
   unpack8(gl, gp);
   unpack8(gh, gq);
 #pragma unroll
   for (int e = 0; e < 8; e++) s = fmaf(p[e], p[e], fmaf(q[e], q[e], s));
-  s = group_sum<LPH>(s);
+  s = over_lanes<LPH, false>(s);
   if (!active) return;
   const float r = rsqrtf(s / (float)a.head_dim + a.eps);
 #pragma unroll
   for (int e = 0; e < 8; e++) {
     const float np = p[e] * r * gp[e], nq = q[e] * r * gq[e];
-    p[e] = a.rope_table ? np * cs[e] - nq * sn[e] : np;
-    q[e] = a.rope_table ? nq * cs[e] + np * sn[e] : nq;
+    p[e] = ROTATE ? np * cs[e] - nq * sn[e] : np;
+    q[e] = ROTATE ? nq * cs[e] + np * sn[e] : nq;
   }
   bf16_t* o = (bf16_t*)a.y + t * a.y_stride + (int64_t)h * a.head_dim + i0;
   store16<PAST>(o, pack8(p));
@@ -390,15 +402,14 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
 // dx = r (d - n mean(d n)), dgamma = sum over tokens and heads of g n.  r is formed anew from x, which has to be read anyway.  The
 // first q_blocks workgroups take the query heads, the others the key heads, each walking over its share of the tokens with the sums of
 // g n in registers; it leaves one row of partial sums.
-template <int LPH, int HEADS, bool PAST>
+template <int LPH, bool ROTATE, bool PAST>
 __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* __restrict__ partial_q, float* __restrict__ partial_k, int q_blocks) {
   constexpr int GROUPS = 256 / LPH;
-  __shared__ float part[4][LPH][17];
+  __shared__ float part[16][256 + 4];   // [element][thread]; the sums are read a row of them at a time
   const bool is_q = (int)blockIdx.x < q_blocks;
   const int block = is_q ? blockIdx.x : blockIdx.x - q_blocks, blocks = is_q ? q_blocks : gridDim.x - q_blocks;
-  const int n_heads = is_q ? a.n_q_heads : a.n_kv_heads, col = is_q ? 0 : a.n_q_heads * a.head_dim;
-  const int per_token = (n_heads + HEADS - 1) / HEADS;
-  const int l = threadIdx.x % LPH, i0 = l * 8, half = a.head_dim >> 1;
+  const int l = threadIdx.x % LPH, i0 = l * 8, half = a.head_dim >> 1, col = (is_q ? 0 : a.n_q_heads * a.head_dim) + i0;
+  const uint32_t n_heads = is_q ? a.n_q_heads : a.n_kv_heads, units = (uint32_t)a.t * n_heads;   // below 2^28, as forward
   const bool active = i0 < half;
   float g[16], dg[16];
 #pragma unroll
@@ -409,85 +420,68 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
     load8(gamma + half, g + 8);
   }
   const float inv = 1.f / (float)a.head_dim;
-  const uint32_t units = (uint32_t)a.t * per_token;   // below 2^28, as forward
   for (uint32_t unit = block * GROUPS + threadIdx.x / LPH; unit < units; unit += blocks * GROUPS) {
-    const uint32_t token = unit / (uint32_t)per_token;
-    const int64_t t = token;
-    const int u = (int)(unit - token * per_token);
-    const int64_t at = a.rope_table ? a.pos[t] : 0;   // first, as forward
-    uint4 xl[HEADS], xh[HEADS], dl[HEADS], dh[HEADS];
-#pragma unroll
-    for (int j = 0; j < HEADS; j++) {
-      const int h = u + j * per_token;
-      xl[j] = xh[j] = dl[j] = dh[j] = make_uint4(0, 0, 0, 0);
-      if (active && h < n_heads) {
-        const int64_t c = col + (int64_t)h * a.head_dim + i0;
-        const bf16_t *px = (const bf16_t*)a.x + t * a.x_stride + c, *pd = (const bf16_t*)a.dy + t * a.dy_stride + c;
-        xl[j] = load16_once(px);
-        xh[j] = load16_once(px + half);
-        dl[j] = load16_once(pd);
-        dh[j] = load16_once(pd + half);
-      }
+    const uint32_t token = unit / n_heads;
+    const int64_t t = token, c = col + (int64_t)(unit - token * n_heads) * a.head_dim, at = ROTATE ? a.pos[t] : 0;   // the position first, as forward
+    uint4 xl = make_uint4(0, 0, 0, 0), xh = xl, dl = xl, dh = xl;
+    if (active) {
+      const bf16_t *px = (const bf16_t*)a.x + t * a.x_stride + c, *pd = (const bf16_t*)a.dy + t * a.dy_stride + c;
+      xl = load16_once(px);
+      xh = load16_once(px + half);
+      dl = load16_once(pd);
+      dh = load16_once(pd + half);
     }
     float cs[8], sn[8];
-    rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
+    if (ROTATE) rotary_factors(a.rope_table, at, a.n_pos, a.head_dim, i0, active, cs, sn);
+    float x[16], d[16], s = 0.f;
+    unpack8(xl, x);
+    unpack8(xh, x + 8);
+    unpack8(dl, d);
+    unpack8(dh, d + 8);
+    if (ROTATE)
 #pragma unroll
-    for (int j = 0; j < HEADS; j++) {
-      const int h = u + j * per_token;
-      if (h >= n_heads) break;
-      float x[16], d[16], s = 0.f;
-      unpack8(xl[j], x);
-      unpack8(xh[j], x + 8);
-      unpack8(dl[j], d);
-      unpack8(dh[j], d + 8);
-      if (a.rope_table)
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const float p = d[e], q = d[e + 8];
-          d[e] = p * cs[e] + q * sn[e];
-          d[e + 8] = q * cs[e] - p * sn[e];
-        }
-#pragma unroll
-      for (int e = 0; e < 16; e++) s = fmaf(x[e], x[e], s);
-      const float r = rsqrtf(group_sum<LPH>(s) * inv + a.eps);
-      float m = 0.f;
-#pragma unroll
-      for (int e = 0; e < 16; e++) {
-        x[e] *= r;
-        const float dn = d[e] * x[e];
-        dg[e] += dn;
-        d[e] *= g[e];
-        m = fmaf(dn, g[e], m);
+      for (int e = 0; e < 8; e++) {
+        const float p = d[e], q = d[e + 8];
+        d[e] = p * cs[e] + q * sn[e];
+        d[e + 8] = q * cs[e] - p * sn[e];
       }
-      m = group_sum<LPH>(m) * inv;
-      if (!active) continue;
-      float o[16];
 #pragma unroll
-      for (int e = 0; e < 16; e++) o[e] = r * (d[e] - x[e] * m);
-      bf16_t* p = (bf16_t*)a.y + t * a.y_stride + col + (int64_t)h * a.head_dim + i0;
-      store16<PAST>(p, pack8(o));
-      store16<PAST>(p + half, pack8(o + 8));
+    for (int e = 0; e < 16; e++) s = fmaf(x[e], x[e], s);
+    const float r = rsqrtf(over_lanes<LPH, false>(s) * inv + a.eps);
+    float m = 0.f;
+#pragma unroll
+    for (int e = 0; e < 16; e++) {
+      x[e] *= r;
+      const float dn = d[e] * x[e];
+      dg[e] += dn;
+      d[e] *= g[e];
+      m = fmaf(dn, g[e], m);
     }
+    m = over_lanes<LPH, false>(m) * inv;
+    if (!active) continue;
+#pragma unroll
+    for (int e = 0; e < 16; e++) d[e] = r * (d[e] - x[e] * m);
+    bf16_t* p = (bf16_t*)a.y + t * a.y_stride + c;
+    store16<PAST>(p, pack8(d));
+    store16<PAST>(p + half, pack8(d + 8));
   }
-  // lane groups of a wavefront, then the four wavefronts
 #pragma unroll
-  for (int e = 0; e < 16; e++)
-#pragma unroll
-    for (int o = 32; o >= LPH; o >>= 1) dg[e] += __shfl_xor(dg[e], o, 64);
-  if ((threadIdx.x & 63) < LPH)
-#pragma unroll
-    for (int e = 0; e < 16; e++) part[threadIdx.x >> 6][l][e] = dg[e];
+  for (int e = 0; e < 16; e++) part[e][threadIdx.x] = dg[e];
   __syncthreads();
+  // a thread adds up an element and a lane of the head over the lane groups
   float* out = (is_q ? partial_q : partial_k) + (int64_t)block * a.head_dim;
-  for (int c = threadIdx.x; c < a.head_dim; c += 256) {
-    const int i = c < half ? c : c - half, e = (i & 7) + (c < half ? 0 : 8), k = i >> 3;
-    out[c] = (part[0][k][e] + part[1][k][e]) + (part[2][k][e] + part[3][k][e]);
+  for (int c = threadIdx.x; c < 16 * LPH; c += 256) {
+    const int e = c / LPH, k = c % LPH, at = k * 8 + (e & 7) + (e < 8 ? 0 : half);
+    float sum = 0.f;
+#pragma unroll 8
+    for (int g = 0; g < GROUPS; g++) sum += part[e][g * LPH + k];
+    if (k * 8 < half) out[at] = sum;
   }
 }
 
 // ---------------------------------------------------------------------------------------------
 // Loss over the vocabulary and its gradient, the row read once: GROUP threads hold up to NV vectors of eight logits each in registers
-// from the maximum to the gradient; what a longer row has beyond GROUP * NV vectors is read again for the gradient.  With the
+// from the maximum to the gradient; of a longer row the vectors behind the first GROUP * NV are read again for the gradient.  With the
 // maximum m and L = log2(e):  s = sum 2^((x - m) L), loss = log2(s) / L + (m - x[target]), gradient = 2^((x - m) L - log2(s) + log2 |weight|)
 // with the weight's sign, less the weight at the target.  Every thread sums against its own maximum, so that one exchange joins (m, s) of all.
 // (x L - m L in one instruction would lose rows of the type's lowest value: m L is beyond the largest number.)
@@ -574,51 +568,39 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
       for (int c = tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
     return;
   }
-  Logits8<E> v[NV];
-#pragma unroll
-  for (int j = 0; j < NV; j++) {
-    const int c = tid + j * GROUP;
-    v[j].none();
-    if (c < nvec) v[j].load(x + (int64_t)c * 8);
-  }
   const float xt = tid == 0 && target < a.vocab ? (sizeof(E) == 2 ? __uint_as_float((uint32_t)((const bf16_t*)x)[target] << 16) : ((const float*)x)[target])
                                                 : __uint_as_float(0x7fc00000u);
-  if (tail)
+  constexpr int STEP = NV * GROUP;
+  Logits8<E> v[NV];
+  float m = -INFINITY, s = 0.f;
+  for (int from = (nvec - 1) / STEP * STEP; from >= 0; from -= STEP) {   // the first vectors last: they are what stays
 #pragma unroll
-    for (int j = 0; j < NV; j++)
-      if (tid + j * GROUP == nvec - 1) v[j].keep(tail);
-  float m = largest<NV>(v), s = 0.f;
-  auto add = [&](const Logits8<E>& u, float m) {
-    float f[8];
-    u.get(f);
+    for (int j = 0; j < NV; j++) {
+      const int c = from + tid + j * GROUP;
+      v[j].none();
+      if (c < nvec) v[j].load(x + (int64_t)c * 8);
+    }
+    if (tail)
 #pragma unroll
-    for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f((f[e] - m) * LOG2E);
-    s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
-  };
-  {
+      for (int j = 0; j < NV; j++)
+        if (from + tid + j * GROUP == nvec - 1) v[j].keep(tail);
+    const float n = fmaxf(m, largest<NV>(v));
+    s *= rescale(m, n);
+    m = n;
     const float c = m == -INFINITY ? 0.f : m;          // nothing but -inf: s is 0 of no weight
 #pragma unroll
     for (int j = 0; j < NV; j++) {
       v[j].settle();
-      add(v[j], c);
+      float f[8];
+      v[j].get(f);
+#pragma unroll
+      for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f((f[e] - c) * LOG2E);
+      s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
     }
-  }
-  for (int c = tid + NV * GROUP; c < nvec; c += GROUP) {
-    Logits8<E> u;
-    u.load(x + (int64_t)c * 8);
-    if (tail && c == nvec - 1) u.keep(tail);
-    const float n = fmaxf(m, largest<1>(&u));
-    if (n != m) {
-      s *= rescale(m, n);
-      m = n;
-    }
-    add(u, m == -INFINITY ? 0.f : m);
   }
   // all threads' (m, s) in one (without anything but -inf s ends as 0, and the differences of m below as NaN)
-  float top = m;
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) top = fmaxf(top, __shfl_xor(top, o, 64));
-  s = wave_sum(s * rescale(m, top));
+  float top = over_lanes<64, true>(m);
+  s = over_lanes<64, false>(s * rescale(m, top));
   if (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = make_float2(top, s);
     __syncthreads();
@@ -656,10 +638,13 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     v[j].settle();
     if (tid + j * GROUP < nvec) put(tid + j * GROUP, v[j]);
   }
-  for (int c = tid + NV * GROUP; c < nvec; c += GROUP) {
-    Logits8<E> u;
-    u.load(x + (int64_t)c * 8);
-    put(c, u);
+  for (int from = STEP; from < nvec; from += STEP) {
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+      if (from + tid + j * GROUP < nvec) v[j].load(x + (int64_t)(from + tid + j * GROUP) * 8);
+#pragma unroll
+    for (int j = 0; j < NV; j++)
+      if (from + tid + j * GROUP < nvec) put(from + tid + j * GROUP, v[j]);
   }
   for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
 }
@@ -751,13 +736,13 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
 }
 
 namespace {
-constexpr int QK_HEADS = 2;   // of a token that a lane group of the backward pass takes (1 205 us for 32768 x 40 x 128, 2 194, 4 209)
 int qk_lanes(int head_dim) { return head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
-// Workgroups of the backward pass that take `heads` of `all` heads.
+// Workgroups of the backward pass that take `heads` of `all` heads: a lane group walks over some eight heads, within 1024 to 4096 workgroups
+// for all (32768 x 40 x 128: 1024 219 us, 2048 203, 4096 195; 5125 x 50 x 128: 1024 40.1, 4096 41.2; 8000 x 12 x 256: 1024 32.7, 4096 38.4, every
+// workgroup leaves partial sums).
 int64_t qk_bwd_blocks(int64_t t, int heads, int all, int head_dim) {
-  // up to eight workgroups a CU: 1024 of them 225 us for 32768 x 40 x 128, 2048 194, 4096 199, and more partial sums for fewer tokens
-  const int64_t units = t * ceil_div(heads, QK_HEADS), groups = 256 / qk_lanes(head_dim);
-  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(units, groups), ceil_div((int64_t)2048 * heads, all)));
+  const int64_t groups = 256 / qk_lanes(head_dim), most = std::min<int64_t>(4096, std::max<int64_t>(1024, t * all / (8 * groups)));
+  return std::max<int64_t>(1, std::min<int64_t>(ceil_div(t * heads, groups), ceil_div(most * heads, all)));
 }
 }  // namespace
 
@@ -766,9 +751,14 @@ hipError_t launch_qk_norm_fwd(const QkNormArgs& a, hipStream_t s) {
   const int n_heads = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
   ProfScope prof(PROF_ELEMENTWISE, 4.0 * (double)a.t * n_heads * a.head_dim, s);
   const dim3 grid((unsigned)ceil_div(a.t * n_heads, 256 / lph));
-#define CALL(L, P) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, P>), grid, dim3(256), 0, s, a)
-#define CALL_LPH(P) do { if (lph == 2) CALL(2, P); else if (lph == 4) CALL(4, P); else if (lph == 8) CALL(8, P); else CALL(16, P); } while (0)
-  if (a.t * n_heads * a.head_dim * 2 > NT_BYTES) CALL_LPH(true); else CALL_LPH(false);
+  const bool past = a.t * n_heads * a.head_dim * 2 > NT_BYTES;
+#define CALL(L, R)                                                                                    \
+  do {                                                                                                \
+    if (past) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, R, true>), grid, dim3(256), 0, s, a);         \
+    else hipLaunchKernelGGL((qk_norm_fwd_kernel<L, R, false>), grid, dim3(256), 0, s, a);             \
+  } while (0)
+#define CALL_LPH(R) do { if (lph == 2) CALL(2, R); else if (lph == 4) CALL(4, R); else if (lph == 8) CALL(8, R); else CALL(16, R); } while (0)
+  if (a.rope_table) CALL_LPH(true); else CALL_LPH(false);
 #undef CALL_LPH
 #undef CALL
   return hipGetLastError();
@@ -785,13 +775,15 @@ hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamm
   const bool past = a.t * all * a.head_dim * 2 > NT_BYTES;
   float *pq = nullptr, *pk = nullptr;
   ProfScope prof(PROF_ELEMENTWISE, 6.0 * (double)a.t * all * a.head_dim, s);
-#define CALL(L, BLOCKS, Q)                                                                                                                           \
+#define CALL(L, R, BLOCKS, Q)                                                                                                                         \
   do {                                                                                                                                               \
-    if (past) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS, true>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));           \
-    else hipLaunchKernelGGL((qk_norm_bwd_kernel<L, QK_HEADS, false>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));               \
+    if (past) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, true>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));                  \
+    else hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, false>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));                      \
   } while (0)
+#define CALL_R(R, BLOCKS, Q) \
+  do { if (lph == 2) CALL(2, R, BLOCKS, Q); else if (lph == 4) CALL(4, R, BLOCKS, Q); else if (lph == 8) CALL(8, R, BLOCKS, Q); else CALL(16, R, BLOCKS, Q); } while (0)
 #define CALL_LPH(BLOCKS, Q) \
-  do { if (lph == 2) CALL(2, BLOCKS, Q); else if (lph == 4) CALL(4, BLOCKS, Q); else if (lph == 8) CALL(8, BLOCKS, Q); else CALL(16, BLOCKS, Q); } while (0)
+  do { if (a.rope_table) CALL_R(true, BLOCKS, Q); else CALL_R(false, BLOCKS, Q); } while (0)
   hipError_t e = sums.room((size_t)(bq + bk) * a.head_dim, a.head_dim, {dgamma_q, dgamma_k}, s);
   if (e == hipSuccess) e = sums.take(bq, a.head_dim, {dgamma_q}, s, &pq);
   if (e != hipSuccess) return e;
@@ -801,6 +793,7 @@ hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamm
   if ((e = sums.take(bk, a.head_dim, {dgamma_k}, s, &pk)) != hipSuccess) return e;
   if (shared) CALL_LPH(bk, 0); else CALL_LPH(bq + bk, bq);
 #undef CALL_LPH
+#undef CALL_R
 #undef CALL
   return hipGetLastError();
 }
@@ -816,10 +809,18 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
     if (past) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, true>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);        \
     else hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);            \
   } while (0)
+  // Threads times vectors that hold a row with the least idle and two workgroups a CU at least where that goes; TB/s of what a pass
+  // reads and writes, rows of bf16: 1000 columns 64x2 5.1, 64x4 4.2; 4096 256x2 5.4, 256x4 4.6; 8192 256x4 5.8, 512x4 5.1; 16384 512x4 5.9,
+  // 256x8 5.5; 32000 512x8 5.5, 512x16 5.3, 1024x8 3.6; 65536 512x16 5.4, 1024x8 4.9; 96000 (a third of the row read again) 512x16 5.1, 1024x20 4.4;
+  // 131072 1024x20 4.8, 512x16 4.6; 256000 1024x20 4.7.  fp32: 1000 64x2 5.9; 4096 256x4 5.9; 16384 512x8 6.1, 1024x8 4.6; 65536 1024x10 5.3,
+  // 512x8 4.8; 131072 1024x10 4.6, 512x16 4.3.
   if (logits_fp32) {
-    if (nvec <= 256) CALL(float, 64, 4); else if (nvec <= 2048) CALL(float, 256, 8); else if (nvec <= 4096) CALL(float, 1024, 4); else CALL(float, 1024, 8);
+    if (nvec <= 128) CALL(float, 64, 2); else if (nvec <= 256) CALL(float, 64, 4); else if (nvec <= 1024) CALL(float, 256, 4);
+    else if (nvec <= 4096) CALL(float, 512, 8); else CALL(float, 1024, 10);
   } else {
-    if (nvec <= 256) CALL(bf16_t, 64, 4); else if (nvec <= 2048) CALL(bf16_t, 256, 8); else if (nvec <= 8192) CALL(bf16_t, 1024, 8); else CALL(bf16_t, 1024, 16);
+    if (nvec <= 128) CALL(bf16_t, 64, 2); else if (nvec <= 256) CALL(bf16_t, 64, 4); else if (nvec <= 512) CALL(bf16_t, 256, 2);
+    else if (nvec <= 1024) CALL(bf16_t, 256, 4); else if (nvec <= 2048) CALL(bf16_t, 512, 4); else if (nvec <= 4096) CALL(bf16_t, 512, 8);
+    else if (nvec <= 12288) CALL(bf16_t, 512, 16); else CALL(bf16_t, 1024, 20);
   }
 #undef CALL
   return hipGetLastError();
