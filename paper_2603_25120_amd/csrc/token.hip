@@ -25,8 +25,10 @@ __device__ __forceinline__ void load8(const float* p, float* f) {
 }
 __device__ __forceinline__ void load8(const bf16_t* p, float* f) { unpack8(*reinterpret_cast<const uint4*>(p), f); }
 
-// Results that together exceed the L2 caches (NT_BYTES) are stored past them: nobody finds them there any more, and as ordinary stores
-// they displace what is being read (32768 x 4096 rows of the table 72 -> 50 us; the figures at the kernels have it).
+// Results of NT_BYTES and more, half of the memory-side cache, are stored past the caches: the kernel that reads them next does not find them
+// there, and as ordinary stores they displace what is being read (32768 x 4096 rows of the table 72 -> 50 us).  With that kernel behind the call,
+// us past the caches and not: norm and rotation with the attention that reads it, 84 MB 151 and 145, 126 MB 206 and 194, 168 MB 246 and 247,
+// 252 MB 353 and 359; embedding rows with the norm that reads them, 101 MB 66.5 and 66.8, 134 MB 88 and 91, 201 MB 141 and 144.
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 template <bool PAST>   // (a flag at run time will not do: the compiler makes one ordinary store of both)
 __device__ __forceinline__ void store16(void* p, const uint4& v) {
@@ -40,7 +42,7 @@ __device__ __forceinline__ uint4 load16_once(const void* p) {   // what nobody r
   const u32x4 w = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(p));
   return make_uint4(w[0], w[1], w[2], w[3]);
 }
-constexpr int64_t NT_BYTES = (int64_t)32 << 20;   // eight L2 caches of 4 MB
+constexpr int64_t NT_BYTES = (int64_t)128 << 20;
 
 // What 2, 4, 8, 16 or 64 neighbouring lanes hold, added up or the largest, in all of them: exchanges inside the vector unit (through LDS, as
 // __shfl_xor goes, a step is some fifty cycles).
@@ -660,7 +662,7 @@ hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* id
 #define CALL(E, L, P) hipLaunchKernelGGL((embed_fwd_kernel<E, L, P>), grid, dim3(256), 0, s, (const E*)table, ids, (bf16_t*)y, t, vocab, nvec, y_stride, scale)
 #define CALL_LPR(E, P) \
   do { if (lpr == 8) CALL(E, 8, P); else if (lpr == 16) CALL(E, 16, P); else if (lpr == 32) CALL(E, 32, P); else CALL(E, 64, P); } while (0)
-#define CALL_PAST(E) do { if (t * d * 2 > NT_BYTES) CALL_LPR(E, true); else CALL_LPR(E, false); } while (0)
+#define CALL_PAST(E) do { if (t * d * 2 >= NT_BYTES) CALL_LPR(E, true); else CALL_LPR(E, false); } while (0)
   if (table_fp32) CALL_PAST(float); else CALL_PAST(bf16_t);
 #undef CALL_PAST
 #undef CALL_LPR
@@ -751,7 +753,7 @@ hipError_t launch_qk_norm_fwd(const QkNormArgs& a, hipStream_t s) {
   const int n_heads = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
   ProfScope prof(PROF_ELEMENTWISE, 4.0 * (double)a.t * n_heads * a.head_dim, s);
   const dim3 grid((unsigned)ceil_div(a.t * n_heads, 256 / lph));
-  const bool past = a.t * n_heads * a.head_dim * 2 > NT_BYTES;
+  const bool past = a.t * n_heads * a.head_dim * 2 >= NT_BYTES;
 #define CALL(L, R)                                                                                    \
   do {                                                                                                \
     if (past) hipLaunchKernelGGL((qk_norm_fwd_kernel<L, R, true>), grid, dim3(256), 0, s, a);         \
@@ -772,7 +774,7 @@ size_t qk_norm_bwd_partial_floats(int64_t t, int n_q_heads, int n_kv_heads, int 
 hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamma_k, PartialSums& sums, hipStream_t s) {
   const int all = a.n_q_heads + a.n_kv_heads, lph = qk_lanes(a.head_dim);
   const int64_t bq = qk_bwd_blocks(a.t, a.n_q_heads, all, a.head_dim), bk = qk_bwd_blocks(a.t, a.n_kv_heads, all, a.head_dim);
-  const bool past = a.t * all * a.head_dim * 2 > NT_BYTES;
+  const bool past = a.t * all * a.head_dim * 2 >= NT_BYTES;
   float *pq = nullptr, *pk = nullptr;
   ProfScope prof(PROF_ELEMENTWISE, 6.0 * (double)a.t * all * a.head_dim, s);
 #define CALL(L, R, BLOCKS, Q)                                                                                                                         \
@@ -803,7 +805,7 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   ProfScope prof(PROF_ELEMENTWISE, (double)a.t * ((logits_fp32 ? 4.0 : 2.0) * (double)a.vocab + (a.dlogits ? 2.0 * (double)a.cols : 0.0)), s);
   const int64_t nvec = ceil_div(a.vocab, 8), blocks = nvec <= 256 ? ceil_div(a.t, 4) : a.t;
   const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
-  const bool past = a.dlogits && a.t * a.cols * 2 > NT_BYTES;
+  const bool past = a.dlogits && a.t * a.cols * 2 >= NT_BYTES;
 #define CALL(E, GROUP, NV)                                                                                                  \
   do {                                                                                                                      \
     if (past) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, true>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);        \
