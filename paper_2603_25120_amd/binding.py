@@ -173,11 +173,9 @@ def _check(status: int):
 
 
 def _ptr(t) -> Optional[int]:
-    if t is None:
-        return None
-    if isinstance(t, int):
+    if t is None or isinstance(t, int):
         return t
-    return int(t.data_ptr())
+    return t.data_ptr()
 
 
 def _nbytes(t) -> int:

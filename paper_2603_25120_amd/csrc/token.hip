@@ -404,10 +404,13 @@ __global__ __launch_bounds__(256) void qk_norm_fwd_kernel(QkNormArgs a) {
 // dx = r (d - n mean(d n)), dgamma = sum over tokens and heads of g n.  r is formed anew from x, which has to be read anyway.  The
 // first q_blocks workgroups take the query heads, the others the key heads, each walking over its share of the tokens with the sums of
 // g n in registers; it leaves one row of partial sums.
+// Threads of a workgroup: its row of partial sums stands for more heads than with 256 (5125 x 50 x 128 38.0 and 38.7 us, 32768 x 40 x 128 189
+// and 193; with 1024 37.6 and 190, but 22464 x 32 x 64 63 with 512 and 77).
+constexpr int QK_THREADS = 512;
 template <int LPH, bool ROTATE, bool PAST>
-__global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* __restrict__ partial_q, float* __restrict__ partial_k, int q_blocks) {
-  constexpr int GROUPS = 256 / LPH;
-  __shared__ float part[16][256 + 4];   // [element][thread]; the sums are read a row of them at a time
+__global__ __launch_bounds__(QK_THREADS) void qk_norm_bwd_kernel(QkNormArgs a, float* __restrict__ partial_q, float* __restrict__ partial_k, int q_blocks) {
+  constexpr int GROUPS = QK_THREADS / LPH;
+  __shared__ float part[16][QK_THREADS + 4];   // [element][thread]; the sums are read a row of them at a time
   const bool is_q = (int)blockIdx.x < q_blocks;
   const int block = is_q ? blockIdx.x : blockIdx.x - q_blocks, blocks = is_q ? q_blocks : gridDim.x - q_blocks;
   const int l = threadIdx.x % LPH, i0 = l * 8, half = a.head_dim >> 1, col = (is_q ? 0 : a.n_q_heads * a.head_dim) + i0;
@@ -472,7 +475,7 @@ __global__ __launch_bounds__(256) void qk_norm_bwd_kernel(QkNormArgs a, float* _
   __syncthreads();
   // a thread adds up an element and a lane of the head over the lane groups
   float* out = (is_q ? partial_q : partial_k) + (int64_t)block * a.head_dim;
-  for (int c = threadIdx.x; c < 16 * LPH; c += 256) {
+  for (int c = threadIdx.x; c < 16 * LPH; c += QK_THREADS) {
     const int e = c / LPH, k = c % LPH, at = k * 8 + (e & 7) + (e < 8 ? 0 : half);
     float sum = 0.f;
 #pragma unroll 8
@@ -739,11 +742,11 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
 
 namespace {
 int qk_lanes(int head_dim) { return head_dim <= 32 ? 2 : head_dim <= 64 ? 4 : head_dim <= 128 ? 8 : 16; }
-// Workgroups of the backward pass that take `heads` of `all` heads: a lane group walks over some eight heads, within 1024 to 4096 workgroups
-// for all (32768 x 40 x 128: 1024 219 us, 2048 203, 4096 195; 5125 x 50 x 128: 1024 40.1, 4096 41.2; 8000 x 12 x 256: 1024 32.7, 4096 38.4, every
-// workgroup leaves partial sums).
+// Workgroups of the backward pass that take `heads` of `all` heads: a lane group walks over some eight heads, within 512 to 4096 workgroups
+// for all (32768 x 40 x 128: 2048 195 us, 2560 189; fewer leave the memory idle, more leave more partial sums: 8000 x 12 x 256 with three
+// heads a lane group 38.4, with six 32.7).
 int64_t qk_bwd_blocks(int64_t t, int heads, int all, int head_dim) {
-  const int64_t groups = 256 / qk_lanes(head_dim), most = std::min<int64_t>(4096, std::max<int64_t>(1024, t * all / (8 * groups)));
+  const int64_t groups = QK_THREADS / qk_lanes(head_dim), most = std::min<int64_t>(4096, std::max<int64_t>(512, t * all / (8 * groups)));
   return std::max<int64_t>(1, std::min<int64_t>(ceil_div(t * heads, groups), ceil_div(most * heads, all)));
 }
 }  // namespace
@@ -779,8 +782,8 @@ hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamm
   ProfScope prof(PROF_ELEMENTWISE, 6.0 * (double)a.t * all * a.head_dim, s);
 #define CALL(L, R, BLOCKS, Q)                                                                                                                         \
   do {                                                                                                                                               \
-    if (past) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, true>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));                  \
-    else hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, false>), dim3((unsigned)(BLOCKS)), dim3(256), 0, s, a, pq, pk, (int)(Q));                      \
+    if (past) hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, true>), dim3((unsigned)(BLOCKS)), dim3(QK_THREADS), 0, s, a, pq, pk, (int)(Q));                  \
+    else hipLaunchKernelGGL((qk_norm_bwd_kernel<L, R, false>), dim3((unsigned)(BLOCKS)), dim3(QK_THREADS), 0, s, a, pq, pk, (int)(Q));                      \
   } while (0)
 #define CALL_R(R, BLOCKS, Q) \
   do { if (lph == 2) CALL(2, R, BLOCKS, Q); else if (lph == 4) CALL(4, R, BLOCKS, Q); else if (lph == 8) CALL(8, R, BLOCKS, Q); else CALL(16, R, BLOCKS, Q); } while (0)
