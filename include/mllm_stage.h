@@ -401,15 +401,17 @@ mllm_status_t mllm_op_colsum_static(const void* x, float* out, int accumulate, i
  * The token side of a language model: what a training step does in front of the first decoder stage and behind the last
  * one (the head's products are mllm_op_gemm and mllm_op_linear_bwd), and the per-head QK normalisation of a decoder or encoder
  * layer.  Row strides are in elements and multiples of 8; bf16 and fp32 matrices start on 16 bytes (MLLM_ERR_UNSUPPORTED
- * otherwise).  None of these calls copies from the host, so all may be captured into a graph.  Sums are fp32 and each bf16 result is rounded once.
+ * otherwise).  None of these calls copies from the host, so all may be captured into a graph; calls that overlap need scratch of their
+ * own.  Sums are fp32 and each bf16 result is rounded once.
  * ------------------------------------------------------------------------------------------ */
 
 /* Token rows of the packed sequence: y [t, d] bf16 = scale * table[ids[i]], table [vocab, d] bf16 (table_fp32 0) or fp32 (1), ids device
  * int32 [t], rows of y y_stride apart, d a multiple of 8.  A row whose id is negative names no token (the rows of image tokens, which
- * the connector fills) and becomes zero; an id at or beyond vocab reads nothing and makes its row NaN.  y must not overlap the table. */
+ * the connector fills) and becomes zero; an id at or beyond vocab reads nothing and makes its row NaN.  y must not overlap the table.
+ * t and vocab are at most 2^30, d 2^20. */
 mllm_status_t mllm_op_embed_fwd(const void* table, int table_fp32, const int32_t* ids, void* y, int64_t t, int64_t vocab,
                                 int64_t d, int64_t y_stride, float scale, void* hip_stream);
-/* The table's gradient: dtable [vocab, d] fp32 = scale * (sum of the rows of dy whose id it is, in the order of the tokens);
+/* The table's gradient: dtable [vocab, d] fp32 = scale * (sum of the rows of dy whose id it is), added up in an order that the ids fix;
  * accumulate != 0: added to what dtable holds, rows of other ids untouched.  dy bf16 [t, d], rows dy_stride apart.  Ids outside
  * [0, vocab) contribute nothing.  workspace: mllm_op_embed_bwd_workspace_bytes, 256-byte aligned, contents undefined afterwards (the
  * token lists by id and partial sums; the same bytes serve fewer tokens with the same vocab and d). */
@@ -424,8 +426,8 @@ mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtabl
  * rope_table (device fp32 [n_pos, head_dim] from mllm_op_rope_table), rotated in half-split pairs by the angle of pos[row] (device
  * int32 [t]); without one (rope_table NULL, pos and n_pos ignored) it is only normalised.  A position outside [0, n_pos) reads
  * nothing and makes the row's heads NaN.  y receives the same columns (rows y_stride apart), other columns are not touched; y may be
- * x with the same stride.  head_dim: a multiple of 16, at most 256; t times the heads
- * stays below 2^28. */
+ * x with the same stride and must not overlap x otherwise.  head_dim: a multiple of 16, at most 256; t times the heads stays
+ * below 2^28. */
 mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const void* gamma_k, void* y, const int32_t* pos,
                                        const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
                                        int32_t head_dim, int64_t x_stride, int64_t y_stride, float eps, void* hip_stream);
@@ -446,8 +448,9 @@ mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void
  *   loss [t] fp32 = log(sum over j < vocab of exp(logits[i][j])) - logits[i][targets[i]], 0 where the target is negative
  *   dlogits [t, cols] bf16 = scale * dloss[i] * (softmax(logits[i]) - onehot(targets[i])), rows with a negative target and columns from
  *   vocab on 0; rows dlogits_stride apart; NULL: the loss alone.  dloss fp32 [t], the weight of every row's loss; NULL: 1.
- * dlogits may be logits (bf16, same stride).  The logits of a row with a negative target are not read.  Logits of -inf have probability 0
- * (a target among them: loss +inf); a row that is all -inf, holds +inf or NaN, or whose target is at or beyond vocab gives NaN. */
+ * dlogits may be logits (bf16, same stride) and must not overlap them otherwise.  The logits of a row with a negative target are not
+ * read.  Logits of -inf have probability 0 (a target among them: loss +inf); a row that is all -inf, holds +inf or NaN, or whose target is
+ * at or beyond vocab gives NaN. */
 mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* targets, const float* dloss, float* loss,
                            void* dlogits, int64_t t, int32_t vocab, int32_t cols, int64_t logits_stride, int64_t dlogits_stride,
                            float scale, void* hip_stream);
@@ -555,7 +558,7 @@ mllm_status_t mllm_optimize_parallelism(const mllm_module_profile_t* enc, const 
  * (0 / 1 / 2: the 256x256- and 224x256-tile GEMM kernel in its Y=X.W / dX / dW layouts, 1 also every launch that forms dX and dW together
  * unless both are in 128x128 tiles or quarters of them (then 6): its FLOPs are those of both, its tiles may be 256, 224 or 192 x 256 and
  * 128x128; 3 attention forward,
- * 4 attention backward, 5 the norm / rotary / activation / reduction / copy kernels, 6 the
+ * 4 attention backward, 5 the norm / rotary / activation / reduction / copy / embedding / loss kernels, 6 the
  * 128x128- and 64x64-tile GEMM kernels in any layout, 7 the 192x256-tile form of the large GEMM kernel in any
  * layout): launches[8], milliseconds[8] and work[8] (algorithmic FLOPs for the GEMM and attention
  * classes, algorithmic bytes for class 5) are host arrays.

@@ -461,12 +461,13 @@ static mllm_status_t check_rows(const char* name, const void* p, int64_t width, 
     const mllm_status_t r_ = (expr);       \
     if (r_ != MLLM_OK) return r_;          \
   } while (0)
-// Rows are counted in int32 in the kernels' lists.
 constexpr int64_t MAX_ROWS = INT32_MAX;
+// The embedding's tokens and ids: int32 in the kernels' lists, and fewer than 2^32 threads in a launch.
+constexpr int64_t MAX_TOKENS = 1 << 30, MAX_VOCAB = 1 << 30, MAX_WIDTH = 1 << 20;
 
 static mllm_status_t check_embed(int64_t t, int64_t vocab, int64_t d) {
-  if (t < 0 || t > MAX_ROWS || vocab <= 0 || vocab > (1 << 30)) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^31 - 1 and vocab in 1 .. 2^30");
-  if (d <= 0 || d % 8 || d > (1 << 20)) return op_fail(MLLM_ERR_SHAPE, "d must be a positive multiple of 8, at most 2^20");
+  if (t < 0 || t > MAX_TOKENS || vocab <= 0 || vocab > MAX_VOCAB) return op_fail(MLLM_ERR_SHAPE, "t must be in 0 .. 2^30 and vocab in 1 .. 2^30");
+  if (d <= 0 || d % 8 || d > MAX_WIDTH) return op_fail(MLLM_ERR_SHAPE, "d must be a positive multiple of 8, at most 2^20");
   return MLLM_OK;
 }
 
@@ -481,7 +482,7 @@ mllm_status_t mllm_op_embed_fwd(const void* table, int table_fp32, const int32_t
 }
 
 size_t mllm_op_embed_bwd_workspace_bytes(int64_t t, int64_t vocab, int64_t d) {
-  return t <= 0 || vocab <= 0 || d <= 0 ? 0 : embed_bwd_ws_bytes(t, vocab, d);
+  return t <= 0 || t > MAX_TOKENS || vocab <= 0 || vocab > MAX_VOCAB || d <= 0 || d > MAX_WIDTH ? 0 : embed_bwd_ws_bytes(t, vocab, d);
 }
 
 mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab,
@@ -529,7 +530,7 @@ mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const
 }
 
 size_t mllm_op_qk_norm_rope_bwd_partial_bytes(int64_t t, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
-  return t < 0 || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 ? 0 : qk_norm_bwd_partial_floats(t, n_q_heads, n_kv_heads, head_dim) * 4;
+  return t < 0 || t > MAX_ROWS || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || head_dim > 256 ? 0 : qk_norm_bwd_partial_floats(t, n_q_heads, n_kv_heads, head_dim) * 4;
 }
 
 mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void* gamma_q, const void* gamma_k, void* dx,

@@ -168,6 +168,31 @@ def test_embed_gradient_of_strided_rows_and_of_no_rows(B):
     assert not bool(got.any())
 
 
+def test_embed_gradient_reads_no_row_without_an_id(B):
+    """Rows of image tokens and of ids that no table holds may be anything."""
+    g = gen(17)
+    t, vocab, d = 1500, 900, 136
+    ids, dy = draw_ids("mixed", t, vocab, g), randn(g, t, d)
+    want, bound = embed_grad(dy, ids, vocab, 1.0)
+    dy[(ids < 0) | (ids >= vocab)] = float("nan")
+    got = torch.full((vocab, d), float("nan"), device="cuda")
+    B.mllm_op_embed_bwd(dy, ids, got, t, vocab, d, garbage(B.mllm_op_embed_bwd_workspace_bytes(t, vocab, d)))
+    within(got, want, bound)
+
+
+def test_embed_gradient_with_a_longer_microbatch_s_scratch(B):
+    """A buffer sized for the longest microbatch, its contents left by other calls, serves shorter ones."""
+    g = gen(19)
+    vocab, d = 5000, 264
+    ws = garbage(B.mllm_op_embed_bwd_workspace_bytes(40000, vocab, d))
+    for t in (40000, 3, 33, 9000, 31, 32, 1):
+        ids, dy = draw_ids("zipf", t, vocab, g), randn(g, t, d)
+        got = torch.full((vocab, d), float("nan"), device="cuda")
+        B.mllm_op_embed_bwd(dy, ids, got, t, vocab, d, ws)
+        want, bound = embed_grad(dy, ids, vocab, 1.0)
+        within(got, want, bound, t)
+
+
 def test_embed_gradient_beyond_32_bit_offsets(B):
     vocab, d = 540000, 8192
     got = torch.full((vocab, d), 3.0, device="cuda")
@@ -353,6 +378,22 @@ def test_qk_norm_of_no_rows_and_of_zero_heads(B):
     within(dgq, sums[0], sizes[0])
     p.bwd(None, None, None, dgq, dgk)
     assert not bool(dgq.any()) and not bool(dgk.any())
+
+
+def test_qk_norm_rope_gradients_with_more_scratch(B):
+    """Scratch of a longer microbatch, and a microbatch long enough for lane groups that walk over several heads, repeated bit for bit."""
+    p = Heads(B, 9000, 14, 2, 64, True)
+    want, bound, sums, sizes = p.want_bwd()
+    runs = []
+    for floats in (B.mllm_op_qk_norm_rope_bwd_partial_bytes(p.t, p.hq, p.hkv, p.hd) // 4, B.mllm_op_qk_norm_rope_bwd_partial_bytes(100000, p.hq, p.hkv, p.hd) // 4):
+        partial = torch.full((floats,), float("nan"), device="cuda")
+        dx, dgq, dgk = torch.zeros_like(p.x), torch.empty(p.hd, device="cuda"), torch.empty(p.hd, device="cuda")
+        B.mllm_op_qk_norm_rope_bwd(p.dy, p.x, p.gq, p.gk, dx, dgq, dgk, p.t, p.hq, p.hkv, p.hd, p.stride, p.stride, p.stride, p.eps, partial, **p.rope())
+        runs.append((dx, dgq, dgk))
+    within(p.heads(dx), want, bound)
+    within(dgq, sums[0], sizes[0])
+    within(dgk, sums[1], sizes[1])
+    assert all(torch.equal(a, b) for a, b in zip(*runs))
 
 
 # ---------------------------------------------------------------------------------------------
