@@ -557,7 +557,8 @@ __device__ __forceinline__ float largest(const Logits8<float>* v) {
 // What a sum against the maximum `from` is worth against `to`, at or above it; a sum of nothing but -inf is none.
 __device__ __forceinline__ float rescale(float from, float to) { return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * LOG2E); }
 
-template <typename E, int GROUP, int NV, bool PAST>
+// PARTS: grid z workgroups a row, each of which reads all of it for the sums and forms one step's gradient (1: all of it).
+template <typename E, int GROUP, int NV, bool PAST, bool PARTS>
 __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArgs a) {
   constexpr int BLOCK = GROUP < 256 ? 256 : GROUP, WAVES = GROUP / 64;
   __shared__ float2 wave_sums[WAVES];
@@ -567,10 +568,11 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
   const int32_t target = a.targets[row];
   const E* x = (const E*)a.logits + row * a.stride;
   bf16_t* out = a.dlogits ? (bf16_t*)a.dlogits + row * a.dstride : nullptr;
+  const int part = PARTS ? blockIdx.z : 0, parts = PARTS ? gridDim.z : 1;
   if (target < 0) {
-    if (tid == 0) a.loss[row] = 0.f;
+    if (tid == 0 && part == 0) a.loss[row] = 0.f;
     if (out)
-      for (int c = tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
+      for (int c = part * GROUP + tid; c < a.cols >> 3; c += parts * GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
     return;
   }
   const float xt = tid == 0 && target < a.vocab ? (sizeof(E) == 2 ? __uint_as_float((uint32_t)((const bf16_t*)x)[target] << 16) : ((const float*)x)[target])
@@ -618,7 +620,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
 #pragma unroll
     for (int i = 0; i < WAVES; i++) s += w[i].y * rescale(w[i].x, top);
   }
-  if (tid == 0) a.loss[row] = (float)((double)log2f(s) * (1.0 / (double)LOG2E) + ((double)top - (double)xt));
+  if (tid == 0 && part == 0) a.loss[row] = (float)((double)log2f(s) * (1.0 / (double)LOG2E) + ((double)top - (double)xt));
   if (!out) return;
   const float weight = a.scale * (a.dloss ? a.dloss[row] : 1.f), size = fabsf(weight);
   const uint32_t sign = weight < 0.f ? 0x80008000u : 0u;
@@ -638,12 +640,16 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     r.x ^= sign; r.y ^= sign; r.z ^= sign; r.w ^= sign;
     store16<PAST>(out + (int64_t)c * 8, r);
   };
+  if (part == 0) {
 #pragma unroll
-  for (int j = 0; j < NV; j++) {
-    v[j].settle();
-    if (tid + j * GROUP < nvec) put(tid + j * GROUP, v[j]);
+    for (int j = 0; j < NV; j++) {
+      v[j].settle();
+      if (tid + j * GROUP < nvec) put(tid + j * GROUP, v[j]);
+    }
+    for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
+    if (PARTS && parts > 1) return;
   }
-  for (int from = STEP; from < nvec; from += STEP) {
+  for (int from = PARTS && part > 0 ? part * STEP : STEP; from < nvec; from += PARTS && parts > 1 ? nvec : STEP) {
 #pragma unroll
     for (int j = 0; j < NV; j++)
       if (from + tid + j * GROUP < nvec) v[j].load(x + (int64_t)(from + tid + j * GROUP) * 8);
@@ -651,7 +657,6 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     for (int j = 0; j < NV; j++)
       if (from + tid + j * GROUP < nvec) put(from + tid + j * GROUP, v[j]);
   }
-  for (int c = nvec + tid; c < a.cols >> 3; c += GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
 }
 
 }  // namespace
@@ -807,19 +812,29 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   if (a.t == 0) return hipSuccess;
   ProfScope prof(PROF_ELEMENTWISE, (double)a.t * ((logits_fp32 ? 4.0 : 2.0) * (double)a.vocab + (a.dlogits ? 2.0 * (double)a.cols : 0.0)), s);
   const int64_t nvec = ceil_div(a.vocab, 8), blocks = nvec <= 256 ? ceil_div(a.t, 4) : a.t;
-  const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
+  dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
   const bool past = a.dlogits && a.t * a.cols * 2 >= NT_BYTES;
 #define CALL(E, GROUP, NV)                                                                                                  \
   do {                                                                                                                      \
-    if (past) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, true>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);        \
-    else hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);            \
+    if (past) hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, true, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a); \
+    else hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, false, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);     \
   } while (0)
   // Threads times vectors that hold a row with the least idle and two workgroups a CU at least where that goes; TB/s of what a pass
   // reads and writes, rows of bf16: 1000 columns 64x2 5.1, 64x4 4.2; 4096 256x2 5.4, 256x4 4.6; 8192 256x4 5.8, 512x4 5.1; 16384 512x4 5.9,
   // 256x8 5.5; 32000 512x8 5.5, 512x16 5.3, 1024x8 3.6; 65536 512x16 5.4, 1024x8 4.9; 96000 (a third of the row read again) 512x16 5.1, 1024x20 4.4;
   // 131072 1024x20 4.8, 512x16 4.6; 256000 1024x20 4.7.  fp32: 1000 64x2 5.9; 4096 256x4 5.9; 16384 512x8 6.1, 1024x8 4.6; 65536 1024x10 5.3,
   // 512x8 4.8; 131072 1024x10 4.6, 512x16 4.3.
-  if (logits_fp32) {
+  // Few long rows: as many workgroups a row as it has steps, while every one has a CU to itself.  A lone workgroup is bound by its own exponentials,
+  // two a logit, of which this spares it most of the second (131072 logits, one row 18.0 -> 14.2 us, fp32 17.7 -> 11.5, 64 rows 21.5 -> 17.3;
+  // 260000, 64 rows 37.4 -> 25.7).  Not over the logits themselves, which the other workgroups of the row still read.
+  const int64_t parts = ceil_div(nvec, logits_fp32 ? 4 * 1024 : 8 * 1024);
+  if (parts > 1 && a.t * parts <= 256) {
+    if (a.dlogits && a.dlogits != a.logits) grid.z = (unsigned)parts;
+    if (logits_fp32)
+      hipLaunchKernelGGL((xent_kernel<float, 1024, 4, false, true>), grid, dim3(1024), 0, s, a);
+    else
+      hipLaunchKernelGGL((xent_kernel<bf16_t, 1024, 8, false, true>), grid, dim3(1024), 0, s, a);
+  } else if (logits_fp32) {
     if (nvec <= 128) CALL(float, 64, 2); else if (nvec <= 256) CALL(float, 64, 4); else if (nvec <= 1024) CALL(float, 256, 4);
     else if (nvec <= 4096) CALL(float, 512, 8); else CALL(float, 1024, 10);
   } else {

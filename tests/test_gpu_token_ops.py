@@ -461,6 +461,28 @@ def test_loss_and_gradient(B, t, vocab, cols, fp32):
 
 
 @pytest.mark.parametrize("fp32", [0, 1])
+@pytest.mark.parametrize("t,vocab,cols", [(300, 2043, 2048), (257, 4099, 4104), (260, 8195, 8200), (257, 16401, 16408), (300, 32771, 32784),
+                                          (140, 65537, 65544), (90, 98309, 98312), (100, 140001, 140008), (90, 200003, 200016)])
+def test_loss_and_gradient_of_many_rows(B, t, vocab, cols, fp32):
+    """More rows than the few that several workgroups share, one or two vectors beyond each form's step."""
+    g = gen(t + vocab)
+    logits = randn(g, t, cols, scale=4.0, dtype=torch.float32 if fp32 else torch.bfloat16)
+    logits[:, vocab:] = float("nan")
+    targets = torch.randint(0, vocab, (t,), generator=g, device="cuda", dtype=torch.int32)
+    targets[::5], targets[-1], logits[7] = -1, vocab - 1, -float("inf")
+    logits[7, vocab - 1] = 1.0
+    loss, out = torch.full((t,), float("nan"), device="cuda"), torch.full((t, cols), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_xent(logits, targets, loss, out, t, vocab, cols, scale=-0.6, logits_fp32=fp32)
+    for rows in torch.arange(t, device="cuda").split(50):
+        want, size, grad, bound = want_loss(logits[rows], targets[rows], vocab, -0.6, None)
+        within(loss[rows], want, size, "loss")
+        within(out[rows], grad, bound, "gradient")
+    if not fp32:
+        B.mllm_op_xent(logits, targets, loss, logits, t, vocab, cols, scale=-0.6)
+        assert torch.equal(logits, out)
+
+
+@pytest.mark.parametrize("fp32", [0, 1])
 @pytest.mark.parametrize("vocab,cols", [(50, 56), (3000, 3008), (50257, 50264), (140000, 140000), (300000, 300000)])
 def test_loss_of_masked_and_broken_rows(B, vocab, cols, fp32):
     inf, nan = float("inf"), float("nan")
