@@ -559,6 +559,35 @@ def test_loss_beyond_32_bit_offsets(B):
         assert not bool(part.any())
 
 
+def test_more_rows_than_a_dimension_of_a_grid_holds(B):
+    """Launches that go on in a second dimension, or walk on: 2^20 workgroups along the first."""
+    g = gen(23)
+    t = 4 * (1 << 20) + 4099                                 # four rows a workgroup
+    logits = randn(g, t, 8, scale=2.0)
+    targets = torch.randint(-1, 5, (t,), generator=g, device="cuda", dtype=torch.int32)
+    loss, out = torch.full((t,), float("nan"), device="cuda"), torch.full_like(logits, 7.0)
+    B.mllm_op_xent(logits, targets, loss, out, t, 5, 8)
+    want, size, grad, bound = want_loss(logits, targets, 5, 1.0, None)
+    within(loss, want, size)
+    within(out, grad, bound)
+    t = 2 * (1 << 20) + 77                                   # one row a workgroup
+    logits, targets = logits[:t].expand(t, 8).repeat(1, 257), targets[:t].contiguous()       # 2056 columns
+    loss, out = torch.full((t,), float("nan"), device="cuda"), torch.empty(t, 2056, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_xent(logits, targets, loss, out, t, 2050, 2056)
+    rows = torch.cat([torch.arange(3), torch.arange((1 << 20) - 2, (1 << 20) + 3), torch.arange((1 << 21) - 2, t)]).cuda()
+    want, size, grad, bound = want_loss(logits[rows], targets[rows], 2050, 1.0, None)
+    within(loss[rows], want, size)
+    within(out[rows], grad, bound)
+    assert not bool(loss.isnan().any())
+    del logits, out
+    t = 32 * (1 << 20) + 1003                                # 32 rows of 64 columns or fewer a workgroup
+    table = randn(g, 11, 8)
+    ids = torch.randint(-1, 11, (t,), generator=g, device="cuda", dtype=torch.int32)
+    y = torch.full((t, 8), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_embed_fwd(table, ids, y, t, 11, 8)
+    assert torch.equal(y, torch.cat([table, torch.zeros_like(table[:1])])[ids.long()])
+
+
 # ---------------------------------------------------------------------------------------------
 # streams and graphs
 # ---------------------------------------------------------------------------------------------
