@@ -821,7 +821,7 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   } while (0)
   // Threads times vectors that hold a row with the least idle and two workgroups a CU at least where that goes; TB/s of what a pass
   // reads and writes, rows of bf16: 1000 columns 64x2 5.1, 64x4 4.2; 4096 256x2 5.4, 256x4 4.6; 8192 256x4 5.8, 512x4 5.1; 16384 512x4 5.9,
-  // 256x8 5.5; 32000 512x8 5.5, 512x16 5.3, 1024x8 3.6; 65536 512x16 5.4, 1024x8 4.9; 96000 (a third of the row read again) 512x16 5.1, 1024x20 4.4;
+  // 256x8 5.5; 24000 512x8 5.8, 1024x4 5.2; 27000 and 32000 1024x4 5.9 and 6.1, 512x8 5.5 and 5.6; 65536 512x16 5.4, 1024x8 4.9; 96000 (a third of the row read again) 512x16 5.1, 1024x20 4.4;
   // 131072 1024x20 4.8, 512x16 4.6; 256000 1024x20 4.7.  fp32: 1000 64x2 5.9; 4096 256x4 5.9; 16384 512x8 6.1, 1024x8 4.6; 65536 1024x10 5.3,
   // 512x8 4.8; 131072 1024x10 4.6, 512x16 4.3.
   // Few long rows: as many workgroups a row as it has steps, while every one has a CU to itself.  A lone workgroup is bound by its own exponentials,
@@ -839,8 +839,8 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
     else if (nvec <= 4096) CALL(float, 512, 8); else CALL(float, 1024, 10);
   } else {
     if (nvec <= 128) CALL(bf16_t, 64, 2); else if (nvec <= 256) CALL(bf16_t, 64, 4); else if (nvec <= 512) CALL(bf16_t, 256, 2);
-    else if (nvec <= 1024) CALL(bf16_t, 256, 4); else if (nvec <= 2048) CALL(bf16_t, 512, 4); else if (nvec <= 4096) CALL(bf16_t, 512, 8);
-    else if (nvec <= 12288) CALL(bf16_t, 512, 16); else CALL(bf16_t, 1024, 20);
+    else if (nvec <= 1024) CALL(bf16_t, 256, 4); else if (nvec <= 2048) CALL(bf16_t, 512, 4); else if (nvec <= 3300) CALL(bf16_t, 512, 8);
+    else if (nvec <= 4096) CALL(bf16_t, 1024, 4); else if (nvec <= 12288) CALL(bf16_t, 512, 16); else CALL(bf16_t, 1024, 20);
   }
 #undef CALL
   return hipGetLastError();
