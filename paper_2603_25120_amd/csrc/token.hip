@@ -202,15 +202,70 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void embed_sort_kernel(const int32
   }
 }
 
-// Clears the rows of the ids that no token has (all without `absent`), the workgroups going over the table in one sweep: 131072 rows of 4096
+// Clears the rows of the ids that no token has, the workgroups going over the table in one sweep: 131072 rows of 4096
 // columns 314 us (6.4 TB/s), with a row a wavefront 360; 2999 tokens into 50257 rows of 3584, all launches, 132 and 147.
+// FEW: of up to 64 tokens (or none), whose ids the lanes hold, instead of the bits that the sort leaves.
+template <bool FEW>
 __global__ __launch_bounds__(256) void embed_clear_kernel(float* __restrict__ dtable, const uint64_t* __restrict__ absent, int log2_buckets, int nvec,
-                                                          int64_t n_quads) {
+                                                          int64_t n_quads, const int32_t* __restrict__ ids, int T) {
   const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256, row0 = first / (2 * nvec), quad = first + threadIdx.x;
-  if (quad >= n_quads) return;
-  const int row = (int)row0 + (int)((uint32_t)(quad - row0 * (2 * nvec)) / (uint32_t)(2 * nvec)), at = row >> log2_buckets;
-  if (!absent || absent[(row & ((1 << log2_buckets) - 1)) * SORT_WAVES + (at >> 6)] >> (at & 63) & 1)
-    reinterpret_cast<float4*>(dtable)[quad] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int row = (int)row0 + (int)((uint32_t)(quad - row0 * (2 * nvec)) / (uint32_t)(2 * nvec));
+  bool clear = quad < n_quads;
+  if (FEW) {
+    const int lane = threadIdx.x & 63;
+    const int32_t id = lane < T ? ids[lane] : -1;
+    for (int r = __builtin_amdgcn_readfirstlane(row); r <= __builtin_amdgcn_readlane(row, 63); r++)
+      if (__ballot(id == r) && row == r) clear = false;
+  } else if (clear) {
+    const int at = row >> log2_buckets;
+    clear = absent[(row & ((1 << log2_buckets) - 1)) * SORT_WAVES + (at >> 6)] >> (at & 63) & 1;
+  }
+  if (clear) reinterpret_cast<float4*>(dtable)[quad] = make_float4(0.f, 0.f, 0.f, 0.f);
+}
+
+// Up to 64 tokens: the lanes hold their ids, and the wavefront of an id's first token (and a slice of 512 columns) adds up its rows.  No sorting and no
+// joining: 20 tokens of 256 columns 9.9 us, sorted 14.2; 64 of 2048, added to the gradient, 4 and 14.  (More than a lane's id each would make one
+// wavefront's run of rows too long.)
+constexpr int EMBED_FEW = 64;
+__global__ __launch_bounds__(256) void embed_few_kernel(const bf16_t* __restrict__ dy, const int32_t* __restrict__ ids, float* __restrict__ dtable, int T,
+                                                        int vocab, int slices, int nvec, int64_t ld, float scale, int accumulate) {
+  const int item = blockIdx.x * 4 + (threadIdx.x >> 6), lane = threadIdx.x & 63;
+  const int token = item / slices, v = (item - token * slices) * 64 + lane;
+  if (token >= T) return;
+  const int32_t id = lane < T ? ids[lane] : -1, mine = __builtin_amdgcn_readlane(id, token);
+  if ((uint32_t)mine >= (uint32_t)vocab) return;
+  uint64_t same = __ballot(id == mine);
+  if (__builtin_ctzll(same) != token || v >= nvec) return;
+  float* o = dtable + ((int64_t)mine * nvec + v) * 8;
+  float old[8], acc[8];
+#pragma unroll
+  for (int e = 0; e < 8; e++) old[e] = acc[e] = 0.f;
+  if (accumulate) load8(o, old);
+  while (same) {
+    constexpr int AHEAD = 8;
+    uint4 row[AHEAD];
+    int n = 0;
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      row[j] = make_uint4(0, 0, 0, 0);
+      if (!same) continue;
+      row[j] = load16_once(dy + __builtin_ctzll(same) * ld + (int64_t)v * 8);
+      same &= same - 1;
+      n++;
+    }
+#pragma unroll
+    for (int j = 0; j < AHEAD; j++) {
+      if (j >= n) break;
+      float f[8];
+      unpack8(row[j], f);
+#pragma unroll
+      for (int e = 0; e < 8; e++) acc[e] += f[e];
+    }
+  }
+#pragma unroll
+  for (int e = 0; e < 8; e++) acc[e] = fmaf(scale, acc[e], old[e]);
+  reinterpret_cast<float4*>(o)[0] = make_float4(acc[0], acc[1], acc[2], acc[3]);
+  reinterpret_cast<float4*>(o)[1] = make_float4(acc[4], acc[5], acc[6], acc[7]);
 }
 
 // Adds up a chunk of the sorted tokens: LPR lanes take eight columns each (of a slice of 8 LPR columns) and walk over the chunk's rows, eight
@@ -679,15 +734,14 @@ hipError_t launch_embed_fwd(const void* table, int table_fp32, const int32_t* id
 }
 
 namespace {
-// How the sorted tokens are cut: into chunks of 8, 16 or 32, the shortest that make at most 16384 wavefronts; 32 tokens and fewer are one
-// chunk, and nothing is joined (20 tokens of 256 columns 14.4 us, 16.6 with a launch more).
+// How the sorted tokens are cut: into chunks of 8, 16 or 32, the shortest that make at most 16384 wavefronts.
 struct EmbedCut { int lpr, slices, chunk; int64_t chunks; };
 EmbedCut embed_cut(int64_t t, int64_t d) {
   EmbedCut c;
   const int64_t nvec = d / 8;
   c.lpr = nvec <= 8 ? 8 : nvec <= 16 ? 16 : nvec <= 32 ? 32 : 64;
   c.slices = (int)ceil_div(nvec, c.lpr);
-  c.chunk = t <= 32 ? 32 : 8;
+  c.chunk = 8;
   while (c.chunk < 32 && ceil_div(t, c.chunk) * c.slices * c.lpr > 16384 * 64) c.chunk *= 2;
   c.chunks = ceil_div(t, c.chunk);
   return c;
@@ -701,7 +755,7 @@ size_t align256(size_t n) { return (n + 255) / 256 * 256; }
 }  // namespace
 
 // The token order, its ids, their number, a bit for every id; two rows of partial sums a chunk.  Not less for fewer tokens: shorter chunks are never more
-// than 16384 wavefronts' worth.
+// than 16384 wavefronts' worth.  (EMBED_FEW tokens and fewer leave it alone.)
 size_t embed_bwd_ws_bytes(int64_t t, int64_t vocab, int64_t d) {
   const EmbedCut c = embed_cut(t, d);
   const int64_t most = std::max(ceil_div(t, 32), std::min<int64_t>(ceil_div(t, 8), 16384 * 64 / c.lpr / c.slices));
@@ -712,11 +766,12 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
                             float scale, void* ws, hipStream_t s) {
   const EmbedCut c = embed_cut(t, d);
   const int nvec = (int)(d / 8), log2_buckets = embed_log2_buckets(vocab);
+  const bool few = t <= EMBED_FEW;
   char* w = (char*)ws;
   int32_t *order = (int32_t*)w, *keys = (int32_t*)(w + align256((size_t)t * 4)), *total = (int32_t*)(w + 2 * align256((size_t)t * 4));
   uint64_t* absent = (uint64_t*)((char*)total + 256);
   float* partial = (float*)((char*)absent + ((size_t)SORT_WAVES * 8 << log2_buckets));
-  if (t > 0) {
+  if (!few) {
     ProfScope prof(PROF_ELEMENTWISE, 0.0, s);
     hipLaunchKernelGGL(embed_sort_kernel, dim3(1u << log2_buckets), dim3(64 * SORT_WAVES), 0, s, ids, (int)t, (int)vocab, log2_buckets, order, keys, total,
                        absent);
@@ -724,10 +779,20 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
   if (!accumulate) {
     ProfScope prof(PROF_ELEMENTWISE, (double)vocab * (double)d * 4.0, s);
     const int64_t quads = vocab * nvec * 2, blocks = ceil_div(quads, 256);
-    hipLaunchKernelGGL(embed_clear_kernel, dim3((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID)), dim3(256), 0, s, dtable,
-                       t > 0 ? absent : nullptr, log2_buckets, nvec, quads);
+    const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
+    if (few)
+      hipLaunchKernelGGL(embed_clear_kernel<true>, grid, dim3(256), 0, s, dtable, absent, log2_buckets, nvec, quads, ids, (int)t);
+    else
+      hipLaunchKernelGGL(embed_clear_kernel<false>, grid, dim3(256), 0, s, dtable, absent, log2_buckets, nvec, quads, ids, (int)t);
   }
   if (t == 0) return hipGetLastError();
+  if (few) {
+    ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0, s);
+    const int slices = (int)ceil_div(nvec, 64);
+    hipLaunchKernelGGL(embed_few_kernel, dim3((unsigned)ceil_div(t * slices, 4)), dim3(256), 0, s, (const bf16_t*)dy, ids, dtable, (int)t, (int)vocab, slices,
+                       nvec, dy_stride, scale, accumulate);
+    return hipGetLastError();
+  }
   {
     ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0, s);
     const dim3 grid((unsigned)ceil_div(c.chunks * c.slices, 256 / c.lpr));
@@ -737,7 +802,6 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
     if (c.lpr == 8) CALL(8); else if (c.lpr == 16) CALL(16); else if (c.lpr == 32) CALL(32); else CALL(64);
 #undef CALL
   }
-  if (c.chunks == 1) return hipGetLastError();
   ProfScope prof(PROF_ELEMENTWISE, 0.0, s);
   const int slices = (int)ceil_div(nvec, 32);
   hipLaunchKernelGGL(embed_join_kernel, dim3((unsigned)(ceil_div(c.chunks, 4) * slices)), dim3(256), 0, s, keys, total, dtable, partial, c.chunk,

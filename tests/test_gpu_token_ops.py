@@ -153,6 +153,22 @@ def test_embed_gradient_large(B, t, vocab, d, how):
     within(got, want, bound)
 
 
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("how", ["uniform", "one", "two", "mixed", "none"])
+@pytest.mark.parametrize("t,vocab,d", [(1, 7, 8), (2, 3, 16), (31, 5, 8), (33, 40, 512), (63, 1000, 520), (64, 2, 24), (64, 300000, 8), (64, 33, 2056), (65, 33, 2056)])
+def test_embed_gradient_of_few_tokens(B, t, vocab, d, how, accumulate):
+    g = gen(t + vocab + d)
+    ids, wide, scale = draw_ids(how, t, vocab, g), randn(g, t, d + 8), -1.3
+    dy = wide[:, :d].clone()
+    wide[(ids < 0) | (ids >= vocab)] = float("nan")          # not read
+    before = randn(g, vocab, d, dtype=torch.float32)
+    got = before.clone() if accumulate else torch.full_like(before, float("nan"))
+    B.mllm_op_embed_bwd(wide, ids, got, t, vocab, d, garbage(B.mllm_op_embed_bwd_workspace_bytes(t, vocab, d)), dy_stride=d + 8, scale=scale,
+                        accumulate=accumulate)
+    want, bound = embed_grad(dy, ids, vocab, scale, before if accumulate else None)
+    within(got, want, bound)
+
+
 def test_embed_gradient_of_strided_rows_and_of_no_rows(B):
     g = gen(5)
     t, vocab, d = 200, 40, 72
