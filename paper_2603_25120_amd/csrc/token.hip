@@ -111,7 +111,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ ta
 // in the list without waiting for any other workgroup (32768 tokens 13.6 us, 2999 5.5).  Each of its 16 wavefronts counts a contiguous piece of the tokens per
 // id; from the scan over (id, wavefront) it then places its piece's tokens in their order.  The ids come from L2: 32768 of them are 128 KB.
 // It also leaves a bit for every id of its bucket that no token has: with the gradient overwritten, their rows are cleared
-// (embed_clear_kernel).
+// (embed_sum_kernel).
 // ---------------------------------------------------------------------------------------------
 constexpr int SORT_WAVES = 16, SORT_RANGE = 1024, SORT_IDS = 32;   // RANGE: ids a bucket holds at most
 __device__ __forceinline__ int lanes_below(uint64_t mask) { return __builtin_amdgcn_mbcnt_hi((uint32_t)(mask >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)mask, 0u)); }
@@ -202,24 +202,14 @@ __global__ __launch_bounds__(64 * SORT_WAVES) void embed_sort_kernel(const int32
   }
 }
 
-// Clears the rows of the ids that no token has, the workgroups going over the table in one sweep: 131072 rows of 4096
-// columns 314 us (6.4 TB/s), with a row a wavefront 360; 2999 tokens into 50257 rows of 3584, all launches, 132 and 147.
-// FEW: of up to 64 tokens (or none), whose ids the lanes hold, instead of the bits that the sort leaves.
-template <bool FEW>
-__global__ __launch_bounds__(256) void embed_clear_kernel(float* __restrict__ dtable, const uint64_t* __restrict__ absent, int log2_buckets, int nvec,
-                                                          int64_t n_quads, const int32_t* __restrict__ ids, int T) {
+// Up to 64 tokens, or none: clears the rows of all other ids.  The lanes hold the tokens' ids, the workgroups go over the table in one sweep.
+__global__ __launch_bounds__(256) void embed_clear_kernel(float* __restrict__ dtable, int nvec, int64_t n_quads, const int32_t* __restrict__ ids, int T) {
   const int64_t first = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * 256, row0 = first / (2 * nvec), quad = first + threadIdx.x;
-  const int row = (int)row0 + (int)((uint32_t)(quad - row0 * (2 * nvec)) / (uint32_t)(2 * nvec));
+  const int row = (int)row0 + (int)((uint32_t)(quad - row0 * (2 * nvec)) / (uint32_t)(2 * nvec)), lane = threadIdx.x & 63;
+  const int32_t id = lane < T ? ids[lane] : -1;
   bool clear = quad < n_quads;
-  if (FEW) {
-    const int lane = threadIdx.x & 63;
-    const int32_t id = lane < T ? ids[lane] : -1;
-    for (int r = __builtin_amdgcn_readfirstlane(row); r <= __builtin_amdgcn_readlane(row, 63); r++)
-      if (__ballot(id == r) && row == r) clear = false;
-  } else if (clear) {
-    const int at = row >> log2_buckets;
-    clear = absent[(row & ((1 << log2_buckets) - 1)) * SORT_WAVES + (at >> 6)] >> (at & 63) & 1;
-  }
+  for (int r = __builtin_amdgcn_readfirstlane(row); r <= __builtin_amdgcn_readlane(row, 63); r++)
+    if (__ballot(id == r) && row == r) clear = false;
   if (clear) reinterpret_cast<float4*>(dtable)[quad] = make_float4(0.f, 0.f, 0.f, 0.f);
 }
 
@@ -273,11 +263,27 @@ __global__ __launch_bounds__(256) void embed_few_kernel(const bf16_t* __restrict
 // when its id ended, each such row was waited for by itself: two microbatches of 32768 tokens, half of them images, 4096 columns, 186 -> 138 us).  Where an id ends, the sum goes to
 // its row of the table; one that began in an earlier chunk, or goes on in the next one, to the partial sums instead: [0][chunk] or
 // [1][chunk].
-template <int LPR>
+// Where the table is overwritten, the workgroups behind the sums' clear the rows of the ids that no token has, in one sweep (a row a wavefront:
+// 360 us for 131072 rows of 4096 columns, 314 so).  The sums wait for scattered rows of dy meanwhile, so that they cost little beside it, provided that they keep
+// few registers, which is why only ACCUMULATE has the table's old rows (76 registers; with the 142 of the other form the clearing has too few
+// wavefronts: two microbatches of 32768 tokens into 131072 rows 594 us, 494 so).  With a launch of its own for the clearing the same are 499 us; 2999 tokens
+// into 50257 rows of 3584 132, 122 so; 300 into 1000 of 512 17 and 13.
+template <int LPR, bool ACCUMULATE>
 __global__ __launch_bounds__(256) void embed_sum_kernel(const bf16_t* __restrict__ dy, const int32_t* __restrict__ order, const int32_t* __restrict__ keys,
                                                         const int32_t* __restrict__ total, float* __restrict__ dtable, float* __restrict__ partial,
-                                                        int chunk, int n_chunks, int slices, int nvec, int64_t ld, float scale, int accumulate) {
+                                                        int chunk, int n_chunks, int slices, int nvec, int64_t ld, float scale, uint32_t sum_blocks,
+                                                        const uint64_t* __restrict__ absent, int log2_buckets, int64_t n_quads) {
   constexpr int AHEAD = 8;
+  if (!ACCUMULATE) {
+    const int64_t block = (int64_t)blockIdx.y * gridDim.x + blockIdx.x - sum_blocks;
+    if (block >= 0) {
+      const int64_t first = block * 256, row0 = first / (2 * nvec), quad = first + threadIdx.x;
+      const int row = (int)row0 + (int)((uint32_t)(quad - row0 * (2 * nvec)) / (uint32_t)(2 * nvec)), at = row >> log2_buckets;
+      if (quad < n_quads && absent[(row & ((1 << log2_buckets) - 1)) * SORT_WAVES + (at >> 6)] >> (at & 63) & 1)
+        reinterpret_cast<float4*>(dtable)[quad] = make_float4(0.f, 0.f, 0.f, 0.f);
+      return;
+    }
+  }
   const uint32_t item = blockIdx.x * (256 / LPR) + threadIdx.x / LPR;
   const int c = (int)(item / (uint32_t)slices), v = (int)(item - (uint32_t)c * slices) * LPR + threadIdx.x % LPR;
   const int N = *total;
@@ -303,7 +309,7 @@ __global__ __launch_bounds__(256) void embed_sum_kernel(const bf16_t* __restrict
     for (int j = 0; j < AHEAD; j++) {
 #pragma unroll
       for (int e = 0; e < 8; e++) old[j][e] = 0.f;
-      if (accumulate && i + j < n && key[j] != (i + j + 1 < n ? key[j + 1] : behind)) load8(dtable + ((int64_t)key[j] * nvec + v) * 8, old[j]);
+      if (ACCUMULATE && i + j < n && key[j] != (i + j + 1 < n ? key[j + 1] : behind)) load8(dtable + ((int64_t)key[j] * nvec + v) * 8, old[j]);
     }
 #pragma unroll
     for (int j = 0; j < AHEAD; j++) {
@@ -776,14 +782,11 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
     hipLaunchKernelGGL(embed_sort_kernel, dim3(1u << log2_buckets), dim3(64 * SORT_WAVES), 0, s, ids, (int)t, (int)vocab, log2_buckets, order, keys, total,
                        absent);
   }
-  if (!accumulate) {
+  const int64_t quads = vocab * nvec * 2, clear_blocks = accumulate ? 0 : ceil_div(quads, 256);
+  if (few && !accumulate) {
     ProfScope prof(PROF_ELEMENTWISE, (double)vocab * (double)d * 4.0, s);
-    const int64_t quads = vocab * nvec * 2, blocks = ceil_div(quads, 256);
-    const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
-    if (few)
-      hipLaunchKernelGGL(embed_clear_kernel<true>, grid, dim3(256), 0, s, dtable, absent, log2_buckets, nvec, quads, ids, (int)t);
-    else
-      hipLaunchKernelGGL(embed_clear_kernel<false>, grid, dim3(256), 0, s, dtable, absent, log2_buckets, nvec, quads, ids, (int)t);
+    const dim3 grid((unsigned)std::min(clear_blocks, MAX_GRID), (unsigned)ceil_div(clear_blocks, MAX_GRID));
+    hipLaunchKernelGGL(embed_clear_kernel, grid, dim3(256), 0, s, dtable, nvec, quads, ids, (int)t);
   }
   if (t == 0) return hipGetLastError();
   if (few) {
@@ -794,12 +797,18 @@ hipError_t launch_embed_bwd(const void* dy, const int32_t* ids, float* dtable, i
     return hipGetLastError();
   }
   {
-    ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0, s);
-    const dim3 grid((unsigned)ceil_div(c.chunks * c.slices, 256 / c.lpr));
-#define CALL(L)                                                                                                                                  \
-  hipLaunchKernelGGL((embed_sum_kernel<L>), grid, dim3(256), 0, s, (const bf16_t*)dy, order, keys, total, dtable, partial, c.chunk, (int)c.chunks, \
-                     c.slices, nvec, dy_stride, scale, accumulate)
-    if (c.lpr == 8) CALL(8); else if (c.lpr == 16) CALL(16); else if (c.lpr == 32) CALL(32); else CALL(64);
+    ProfScope prof(PROF_ELEMENTWISE, (double)t * (double)d * 2.0 + (accumulate ? 0.0 : (double)vocab * (double)d * 4.0), s);
+    // The sums' workgroups all in the grid's first row.
+    const int64_t sum_blocks = ceil_div(c.chunks * c.slices, 256 / c.lpr), blocks = sum_blocks + clear_blocks;
+    const int64_t along = std::max(sum_blocks, std::min(blocks, MAX_GRID));
+    const dim3 grid((unsigned)along, (unsigned)ceil_div(blocks, along));
+#define CALL(L, A)                                                                                                                                  \
+  hipLaunchKernelGGL((embed_sum_kernel<L, A>), grid, dim3(256), 0, s, (const bf16_t*)dy, order, keys, total, dtable, partial, c.chunk, (int)c.chunks, \
+                     c.slices, nvec, dy_stride, scale, (uint32_t)sum_blocks, absent, log2_buckets, quads)
+#define CALL_LPR(A) \
+  do { if (c.lpr == 8) CALL(8, A); else if (c.lpr == 16) CALL(16, A); else if (c.lpr == 32) CALL(32, A); else CALL(64, A); } while (0)
+    if (accumulate) CALL_LPR(true); else CALL_LPR(false);
+#undef CALL_LPR
 #undef CALL
   }
   ProfScope prof(PROF_ELEMENTWISE, 0.0, s);

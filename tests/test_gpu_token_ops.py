@@ -604,6 +604,22 @@ def test_more_rows_than_a_dimension_of_a_grid_holds(B):
     assert torch.equal(y, torch.cat([table, torch.zeros_like(table[:1])])[ids.long()])
 
 
+@pytest.mark.parametrize("t", [30, 100, 5000])
+def test_a_table_of_more_than_a_dimension_of_a_grid_is_cleared_but_for_the_ids(B, t):
+    """Where a table is overwritten a workgroup takes 4 KB of it: 2^18 rows of 4096 columns fill the first dimension."""
+    g = gen(31 + t)
+    vocab, d = (1 << 18) + 1500, 4096
+    ids = torch.cat([torch.randint(0, vocab, (t - 12,), generator=g, device="cuda", dtype=torch.int32),
+                     torch.tensor([0, vocab - 1, (1 << 18) - 1, 1 << 18, vocab, -1] * 2, dtype=torch.int32, device="cuda")])
+    dy = torch.randint(-4, 5, (t, d), generator=g, device="cuda").bfloat16()    # whose sums have no roundings
+    want = torch.zeros(vocab, d, device="cuda")
+    held = (ids >= 0) & (ids < vocab)
+    want.index_add_(0, ids[held], dy[held].float())
+    got = torch.full((vocab, d), float("nan"), device="cuda")
+    B.mllm_op_embed_bwd(dy, ids, got, t, vocab, d, garbage(B.mllm_op_embed_bwd_workspace_bytes(t, vocab, d)))
+    assert torch.equal(got, want)
+
+
 # ---------------------------------------------------------------------------------------------
 # streams and graphs
 # ---------------------------------------------------------------------------------------------
