@@ -426,8 +426,8 @@ mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtabl
  * rope_table (device fp32 [n_pos, head_dim] from mllm_op_rope_table), rotated in half-split pairs by the angle of pos[row] (device
  * int32 [t]); without one (rope_table NULL, pos and n_pos ignored) it is only normalised.  A position outside [0, n_pos) reads
  * nothing and makes the row's heads NaN.  y receives the same columns (rows y_stride apart), other columns are not touched; y may be
- * x with the same stride and must not overlap x otherwise.  head_dim: a multiple of 16, at most 256; t times the heads stays
- * below 2^28. */
+ * x with the same stride and must not overlap x otherwise.  head_dim: a multiple of 16, at most 256; n_q_heads and n_kv_heads: at most 65536
+ * each; t times the heads: at most 2^28 - 16. */
 mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const void* gamma_k, void* y, const int32_t* pos,
                                        const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
                                        int32_t head_dim, int64_t x_stride, int64_t y_stride, float eps, void* hip_stream);

@@ -508,8 +508,9 @@ static mllm_status_t check_qk_norm(const QkNormArgs& a) {
   if (a.n_q_heads <= 0 || a.n_kv_heads <= 0 || a.n_q_heads > 65536 || a.n_kv_heads > 65536)
     return op_fail(MLLM_ERR_SHAPE, "n_q_heads and n_kv_heads must be positive, at most 65536");
   const int64_t heads = (int64_t)a.n_q_heads + a.n_kv_heads, width = heads * a.head_dim;
-  // a lane group of up to 16 a head, and fewer than 2^32 threads in a launch
-  if (a.t < 0 || a.t > MAX_ROWS || a.t * heads >= ((int64_t)1 << 28)) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, t times the heads below 2^28");
+  // a lane group of up to 16 a head in whole workgroups of 256, and fewer than 2^32 threads in a launch
+  if (a.t < 0 || a.t > MAX_ROWS || a.t * heads > ((int64_t)1 << 28) - 16)
+    return op_fail(MLLM_ERR_SHAPE, "t must not be negative, t times the heads at most 2^28 - 16");
   if (!(a.eps >= 0.f)) return op_fail(MLLM_ERR_SHAPE, "eps must not be negative");
   if (a.rope_table && a.n_pos < 0) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative");
   CHECK(check_rows("x", a.x, width, a.x_stride));

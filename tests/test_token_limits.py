@@ -1,0 +1,40 @@
+"""Sizes and buffers at the edge of what the token side's entry points take: host only, nothing is launched."""
+import os
+
+import pytest
+
+SHAPE, UNSUPPORTED = 3, 8
+P = 0x10000        # never dereferenced: validation fails first
+
+
+@pytest.fixture(scope="module")
+def B():
+    from paper_2603_25120_amd import binding
+    if not os.path.exists(binding.LIB_PATH):
+        from paper_2603_25120_amd import build
+        build.build()
+    binding.lib()
+    return binding
+
+
+def refused(B, status, call, **kw):
+    with pytest.raises(B.MllmError) as e:
+        call(**kw, stream=1)
+    assert e.value.status == status, str(e.value)
+
+
+def qk(t, hq, hkv, head_dim):
+    width = (hq + hkv) * head_dim
+    return dict(x=P, gamma_q=P, gamma_k=P, t=t, n_q_heads=hq, n_kv_heads=hkv, head_dim=head_dim, x_stride=width, eps=1e-6)
+
+
+@pytest.mark.parametrize("head_dim", [64, 144, 256])
+@pytest.mark.parametrize("hq,hkv", [(2, 1), (4, 1), (14, 1)])
+def test_more_heads_than_a_launch_has_threads_for(B, hq, hkv, head_dim):
+    """Wide heads take 16 lanes: from 2^28 - 15 heads on, whole workgroups of 256 threads hold 2^32 of them, which no launch has."""
+    t = ((1 << 28) - 1) // (hq + hkv)
+    assert t * (hq + hkv) == (1 << 28) - 1
+    width = (hq + hkv) * head_dim
+    refused(B, SHAPE, B.mllm_op_qk_norm_rope_fwd, **qk(t, hq, hkv, head_dim), y=P, y_stride=width)
+    refused(B, SHAPE, B.mllm_op_qk_norm_rope_bwd, **qk(t, hq, hkv, head_dim), dy=P, dx=P, dgamma_q=P, dgamma_k=P + 4096, dy_stride=width,
+            dx_stride=width, partial=P)
