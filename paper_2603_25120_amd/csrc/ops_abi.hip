@@ -500,12 +500,16 @@ mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtabl
   return MLLM_OK;
 }
 
+static bool head_counts_fit(int32_t n_q_heads, int32_t n_kv_heads) {
+  return n_q_heads > 0 && n_kv_heads > 0 && n_q_heads <= 65536 && n_kv_heads <= 65536;
+}
+
 // x, the other matrix that is read (the forward pass has none) and the one that is written.
 static mllm_status_t check_qk_norm(const QkNormArgs& a) {
   if (!a.gamma_q || !a.gamma_k || (a.t > 0 && (!a.x || !a.y || !a.dy))) return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
   if (a.rope_table && a.t > 0 && !a.pos) return op_fail(MLLM_ERR_NULL, "pos is NULL");
   if (a.head_dim <= 0 || a.head_dim % 16 || a.head_dim > 256) return op_fail(MLLM_ERR_UNSUPPORTED, "head_dim must be a multiple of 16, at most 256");
-  if (a.n_q_heads <= 0 || a.n_kv_heads <= 0 || a.n_q_heads > 65536 || a.n_kv_heads > 65536)
+  if (!head_counts_fit(a.n_q_heads, a.n_kv_heads))
     return op_fail(MLLM_ERR_SHAPE, "n_q_heads and n_kv_heads must be positive, at most 65536");
   const int64_t heads = (int64_t)a.n_q_heads + a.n_kv_heads, width = heads * a.head_dim;
   // a lane group of up to 16 a head in whole workgroups of 256, and fewer than 2^32 threads in a launch
@@ -531,7 +535,7 @@ mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const
 }
 
 size_t mllm_op_qk_norm_rope_bwd_partial_bytes(int64_t t, int32_t n_q_heads, int32_t n_kv_heads, int32_t head_dim) {
-  return t < 0 || t > MAX_ROWS || n_q_heads <= 0 || n_kv_heads <= 0 || head_dim <= 0 || head_dim > 256 ? 0 : qk_norm_bwd_partial_floats(t, n_q_heads, n_kv_heads, head_dim) * 4;
+  return t < 0 || t > MAX_ROWS || !head_counts_fit(n_q_heads, n_kv_heads) || head_dim <= 0 || head_dim > 256 ? 0 : qk_norm_bwd_partial_floats(t, n_q_heads, n_kv_heads, head_dim) * 4;
 }
 
 mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void* gamma_q, const void* gamma_k, void* dx,

@@ -38,3 +38,10 @@ def test_more_heads_than_a_launch_has_threads_for(B, hq, hkv, head_dim):
     refused(B, SHAPE, B.mllm_op_qk_norm_rope_fwd, **qk(t, hq, hkv, head_dim), y=P, y_stride=width)
     refused(B, SHAPE, B.mllm_op_qk_norm_rope_bwd, **qk(t, hq, hkv, head_dim), dy=P, dx=P, dgamma_q=P, dgamma_k=P + 4096, dy_stride=width,
             dx_stride=width, partial=P)
+
+
+def test_no_scratch_for_more_heads_than_a_call_takes(B):
+    size = B.mllm_op_qk_norm_rope_bwd_partial_bytes
+    assert size(4, 65536, 65536, 64) > 0
+    for hq, hkv in ((65537, 1), (1, 65537), ((1 << 31) - 1, (1 << 31) - 1)):
+        assert size(4, hq, hkv, 64) == 0
