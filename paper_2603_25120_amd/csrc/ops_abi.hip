@@ -548,6 +548,8 @@ mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void
   CHECK(check_qk_norm(a));
   if (((uintptr_t)dgamma_q | (uintptr_t)dgamma_k | (uintptr_t)partial) % 16)
     return op_fail(MLLM_ERR_UNSUPPORTED, "dgamma_q, dgamma_k and partial must start on 16 bytes");
+  if (dgamma_q != dgamma_k && ranges_overlap(dgamma_q, (int64_t)head_dim * 4, dgamma_k, (int64_t)head_dim * 4))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "dgamma_k may be dgamma_q but not overlap it otherwise");
   PartialSums sums(partial, mllm_op_qk_norm_rope_bwd_partial_bytes(t, n_q_heads, n_kv_heads, head_dim), accumulate);
   OP_TRY(launch_qk_norm_bwd(a, dgamma_q, dgamma_k, sums, (hipStream_t)hip_stream));
   OP_TRY(sums.flush((hipStream_t)hip_stream));

@@ -871,10 +871,22 @@ hipError_t launch_qk_norm_bwd(const QkNormArgs& a, float* dgamma_q, float* dgamm
   if (e == hipSuccess) e = sums.take(bq, a.head_dim, {dgamma_q}, s, &pq);
   if (e != hipSuccess) return e;
   const int64_t bytes = (int64_t)a.head_dim * 4;
-  const bool shared = ranges_overlap(dgamma_q, bytes, dgamma_k, bytes);   // then the second take sends the first sums off
-  if (shared) CALL_LPH(bq, bq);
-  if ((e = sums.take(bk, a.head_dim, {dgamma_k}, s, &pk)) != hipSuccess) return e;
-  if (shared) CALL_LPH(bk, 0); else CALL_LPH(bq + bk, bq);
+  if (ranges_overlap(dgamma_q, bytes, dgamma_k, bytes)) {   // one gain for both: the key heads' sums are added to the query heads' in any case
+    CALL_LPH(bq, bq);
+    if ((e = sums.flush(s)) != hipSuccess) return e;
+    const int accumulate = sums.accumulate;
+    sums.accumulate = 1;
+    e = sums.take(bk, a.head_dim, {dgamma_k}, s, &pk);
+    if (e == hipSuccess) {
+      CALL_LPH(bk, 0);
+      e = sums.flush(s);
+    }
+    sums.accumulate = accumulate;
+    if (e != hipSuccess) return e;
+  } else {
+    if ((e = sums.take(bk, a.head_dim, {dgamma_k}, s, &pk)) != hipSuccess) return e;
+    CALL_LPH(bq + bk, bq);
+  }
 #undef CALL_LPH
 #undef CALL_R
 #undef CALL

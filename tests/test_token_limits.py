@@ -45,3 +45,11 @@ def test_no_scratch_for_more_heads_than_a_call_takes(B):
     assert size(4, 65536, 65536, 64) > 0
     for hq, hkv in ((65537, 1), (1, 65537), ((1 << 31) - 1, (1 << 31) - 1)):
         assert size(4, hq, hkv, 64) == 0
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("offset", [16, 240, -16, -240])
+def test_gains_gradients_that_overlap_in_part(B, offset, accumulate):
+    """One buffer for both takes the sum; 64 values each, some of them shared, mean nothing."""
+    refused(B, UNSUPPORTED, B.mllm_op_qk_norm_rope_bwd, **qk(4, 4, 2, 64), dy=P, dx=P, dgamma_q=2 * P, dgamma_k=2 * P + offset, dy_stride=384,
+            dx_stride=384, partial=P, accumulate=accumulate)
