@@ -549,44 +549,46 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_bwd_kernel(QkNormArgs a, f
 // Loss over the vocabulary and its gradient, the row read once: GROUP threads hold up to NV vectors of eight logits each in registers
 // from the maximum to the gradient; of a longer row the vectors behind the first GROUP * NV are read again for the gradient.  With the
 // maximum m and L = log2(e):  s = sum 2^((x - m) L), loss = log2(s) / L + (m - x[target]), gradient = 2^((x - m) L - log2(s) + log2 |weight|)
-// with the weight's sign, less the weight at the target.  Every thread sums against its own maximum, so that one exchange joins (m, s) of all.
+// with the weight's sign, and |weight| (2^((x - m) L) / s - 1) at the target.  Every thread sums against its own maximum, so that one exchange joins (m, s) of all.
 // (x L - m L in one instruction would lose rows of the type's lowest value: m L is beyond the largest number.)
 // ---------------------------------------------------------------------------------------------
 constexpr float LOG2E = 1.4426950408889634f;
 typedef short s16x2 __attribute__((ext_vector_type(2)));
 typedef unsigned short u16x2 __attribute__((ext_vector_type(2)));
 
+__device__ __forceinline__ float value(bf16_t v) { return __uint_as_float((uint32_t)v << 16); }
+__device__ __forceinline__ float value(float v) { return v; }
+
+// Vectors of the compiler's: of four single words it moved some to other registers behind a load, which waits for each by itself.
+typedef float f32x4 __attribute__((ext_vector_type(4)));
 template <typename E>
 struct Logits8;
 template <>
 struct Logits8<bf16_t> {
-  uint4 u;
-  __device__ __forceinline__ void load(const bf16_t* p) { u = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void none() { u = make_uint4(0xff80ff80u, 0xff80ff80u, 0xff80ff80u, 0xff80ff80u); }   // -inf
-  __device__ __forceinline__ void get(float* f) const { unpack8(u, f); }
+  u32x4 u;
+  __device__ __forceinline__ void load(const bf16_t* p) { u = *reinterpret_cast<const u32x4*>(p); }
+  __device__ __forceinline__ void none() { u = 0xff80ff80u; }   // -inf
+  __device__ __forceinline__ void get(float* f) const { unpack8(make_uint4(u[0], u[1], u[2], u[3]), f); }
   // Keeps the compiler from carrying the unpacked values from one use to the next (129 registers spilled with 16 vectors).
-  __device__ __forceinline__ void settle() { asm volatile("" : "+v"(u.x), "+v"(u.y), "+v"(u.z), "+v"(u.w)); }
+  __device__ __forceinline__ void settle() { asm volatile("" : "+v"(u)); }
   __device__ __forceinline__ void keep(int n) {   // the first n, 1 to 7
-    uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-    for (int i = 0; i < 4; i++) w[i] = 2 * i + 1 < n ? w[i] : 2 * i < n ? (w[i] & 0xffffu) | 0xff800000u : 0xff80ff80u;
-    u = make_uint4(w[0], w[1], w[2], w[3]);
+    for (int i = 0; i < 4; i++) u[i] = 2 * i + 1 < n ? u[i] : 2 * i < n ? (u[i] & 0xffffu) | 0xff800000u : 0xff80ff80u;
   }
 };
 template <>
 struct Logits8<float> {
-  float4 a, b;
-  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const float4*>(p); b = *reinterpret_cast<const float4*>(p + 4); }
-  __device__ __forceinline__ void none() { a = b = make_float4(-INFINITY, -INFINITY, -INFINITY, -INFINITY); }
+  f32x4 a, b;
+  __device__ __forceinline__ void load(const float* p) { a = *reinterpret_cast<const f32x4*>(p); b = *reinterpret_cast<const f32x4*>(p + 4); }
+  __device__ __forceinline__ void none() { a = b = -INFINITY; }
   __device__ __forceinline__ void settle() {}
-  __device__ __forceinline__ void get(float* f) const { f[0] = a.x; f[1] = a.y; f[2] = a.z; f[3] = a.w; f[4] = b.x; f[5] = b.y; f[6] = b.z; f[7] = b.w; }
-  __device__ __forceinline__ void keep(int n) {
-    float f[8];
-    get(f);
+  __device__ __forceinline__ void get(float* f) const {
 #pragma unroll
-    for (int i = 0; i < 8; i++) f[i] = i < n ? f[i] : -INFINITY;
-    a = make_float4(f[0], f[1], f[2], f[3]);
-    b = make_float4(f[4], f[5], f[6], f[7]);
+    for (int i = 0; i < 8; i++) f[i] = i < 4 ? a[i & 3] : b[i & 3];
+  }
+  __device__ __forceinline__ void keep(int n) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) { a[i] = i < n ? a[i] : -INFINITY; b[i] = i + 4 < n ? b[i] : -INFINITY; }
   }
 };
 // The largest of N vectors.  bf16 in pairs without unpacking: among 16-bit integers numbers at or above zero keep their order and are
@@ -596,13 +598,13 @@ __device__ __forceinline__ float largest(const Logits8<bf16_t>* v) {
   s16x2 m = {-32768, -32768};
 #pragma unroll
   for (int j = 0; j < N; j++)
-    for (uint32_t w : {v[j].u.x, v[j].u.y, v[j].u.z, v[j].u.w}) m = __builtin_elementwise_max(m, __builtin_bit_cast(s16x2, w));
+    for (uint32_t w : {v[j].u[0], v[j].u[1], v[j].u[2], v[j].u[3]}) m = __builtin_elementwise_max(m, __builtin_bit_cast(s16x2, w));
   uint32_t top = (uint16_t)(m[0] > m[1] ? m[0] : m[1]);
   if (top & 0x8000u) {
     u16x2 n = {65535, 65535};
 #pragma unroll
     for (int j = 0; j < N; j++)
-      for (uint32_t w : {v[j].u.x, v[j].u.y, v[j].u.z, v[j].u.w}) n = __builtin_elementwise_min(n, __builtin_bit_cast(u16x2, w));
+      for (uint32_t w : {v[j].u[0], v[j].u[1], v[j].u[2], v[j].u[3]}) n = __builtin_elementwise_min(n, __builtin_bit_cast(u16x2, w));
     top = n[0] < n[1] ? n[0] : n[1];
   }
   return __uint_as_float(top << 16);
@@ -611,7 +613,7 @@ template <int N>
 __device__ __forceinline__ float largest(const Logits8<float>* v) {
   float m = -INFINITY;
 #pragma unroll
-  for (int j = 0; j < N; j++) m = fmaxf(fmaxf(fmaxf(fmaxf(v[j].a.x, v[j].a.y), fmaxf(v[j].a.z, v[j].a.w)), fmaxf(fmaxf(v[j].b.x, v[j].b.y), fmaxf(v[j].b.z, v[j].b.w))), m);
+  for (int j = 0; j < N; j++) m = fmaxf(fmaxf(fmaxf(fmaxf(v[j].a[0], v[j].a[1]), fmaxf(v[j].a[2], v[j].a[3])), fmaxf(fmaxf(v[j].b[0], v[j].b[1]), fmaxf(v[j].b[2], v[j].b[3]))), m);
   return m;
 }
 
@@ -636,8 +638,10 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
       for (int c = part * GROUP + tid; c < a.cols >> 3; c += parts * GROUP) store16<PAST>(out + (int64_t)c * 8, make_uint4(0, 0, 0, 0));
     return;
   }
-  const float xt = tid == 0 && target < a.vocab ? (sizeof(E) == 2 ? __uint_as_float((uint32_t)((const bf16_t*)x)[target] << 16) : ((const float*)x)[target])
-                                                : __uint_as_float(0x7fc00000u);
+  int at = target < a.vocab ? target : 0;
+  asm volatile("" : "+v"(at));                         // as a vector load: the next scalar one would wait for it
+  const E raw = x[at];
+  asm volatile("" ::: "memory");                       // requested in front of the row: waited for behind it, it is 0.7 us of a row's 12 (131072 logits)
   constexpr int STEP = NV * GROUP;
   Logits8<E> v[NV];
   float m = -INFINITY, s = 0.f;
@@ -681,6 +685,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
 #pragma unroll
     for (int i = 0; i < WAVES; i++) s += w[i].y * rescale(w[i].x, top);
   }
+  const float xt = target < a.vocab ? value(raw) : __uint_as_float(0x7fc00000u);
   if (tid == 0 && part == 0) a.loss[row] = (float)((double)log2f(s) * (1.0 / (double)LOG2E) + ((double)top - (double)xt));
   if (!out) return;
   const float weight = a.scale * (a.dloss ? a.dloss[row] : 1.f), size = fabsf(weight);
@@ -691,9 +696,14 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     u.get(f);
 #pragma unroll
     for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f(fmaf(f[e] - top, LOG2E, shift));
-    if (c == target >> 3)
+    // The target's own is formed without the weight in the exponent, which at a weight of 1/5000 is rounded to 2^-20 of p, and p - 1 of a
+    // confident row is little more (1 - p = 1e-4, 1e-5: off by up to 1.3 and 12 % so, by 0.7 and 4 % now, as a p in fp32 is).  Here, where one
+    // thread comes by: formed ahead by all, 2999 x 50257 fp32 took 1 % longer.
+    if (c == target >> 3) {
+      const float hit = size * fmaf(__builtin_amdgcn_exp2f((xt - top) * LOG2E), __builtin_amdgcn_rcpf(s), -1.f);
 #pragma unroll
-      for (int e = 0; e < 8; e++) f[e] -= e == (target & 7) ? size : 0.f;
+      for (int e = 0; e < 8; e++) f[e] = e == (target & 7) ? hit : f[e];
+    }
     if (tail && c == nvec - 1)
 #pragma unroll
       for (int e = 0; e < 8; e++) f[e] = e < tail ? f[e] : 0.f;

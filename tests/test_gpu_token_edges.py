@@ -1,10 +1,12 @@
 """Calls at the edge of what the token side's entry points document, each against its definition in float64."""
+import math
+
 import pytest
 
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_token_ops import FP32, SHAPES, Heads, within  # noqa: E402
+from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, gen, randn, within  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -32,3 +34,37 @@ def test_one_gradient_for_both_gains(B, t, hq, hkv, hd, rotate):
     within(both, want, bound)
     p.bwd(p.dy, p.x, dx, both, both, accumulate=1)
     within(both, 2 * want, 2 * bound + 4 * (sums[0].abs() + sums[1].abs()) * FP32)      # two more additions
+
+
+# ---------------------------------------------------------------------------------------------
+# loss
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("fp32", [0, 1])
+@pytest.mark.parametrize("t,vocab", [(600, 61), (600, 1000), (600, 2048), (300, 4096), (300, 16000), (300, 32771), (130, 65544), (2, 131072), (130, 131072)])
+def test_target_s_gradient_of_confident_rows(B, t, vocab, fp32):
+    """Probabilities of the target from 1 - 1e-2 to 1 - 1e-5: its gradient is weight * (p - 1), off by what the sum of the row's exponentials
+    is off and by half a step of bf16.  Where the target is the row's maximum its term is 1, the additions that meet it have a half step of 2^-24
+    each, the others count by their share 1 - p."""
+    g, cols, weight = gen(vocab), vocab + -vocab % 8, 1.0 / 5087
+    x = randn(g, t, cols, scale=2.0, dtype=torch.float32)
+    targets = torch.randint(0, vocab, (t,), generator=g, device="cuda", dtype=torch.int32)
+    at = targets.long()[:, None]
+    x.scatter_(1, at, -float("inf"))
+    rest = x[:, :vocab].double().logsumexp(1)
+    x.scatter_(1, at, (rest + math.log(10) * (2 + 3 * torch.rand(t, generator=g, device="cuda"))).float()[:, None])
+    logits = x if fp32 else x.bfloat16()
+    z = logits[:, :vocab].double()
+    assert bool((z.argmax(1) == at[:, 0]).all())
+    short = ((z - z.amax(1, keepdim=True)).exp().scatter(1, at, 0.0)).sum(1)
+    short = short / (1 + short)                              # 1 - p, without a difference
+    loss, out = torch.empty(t, device="cuda"), torch.empty(t, cols, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_xent(logits, targets, loss, out, t, vocab, cols, scale=weight, logits_fp32=fp32)
+    w = float(torch.tensor(weight, dtype=torch.float32))
+    # in a vector 3 and to the sum 1; vectors a thread at most 20, and 2 sums of earlier ones behind each rescaling; 6 among lanes, 16 among wavefronts; 1 / s, p - 1, w
+    threads = 64 if vocab <= 2048 else 256
+    vectors = min(20, -(-vocab // (8 * threads)))
+    depth = 3 + vectors + 2 + 6 + (16 if vocab > 2048 else 0) + 3
+    bound = w * (depth * FP32 + short * 2.0 ** -14) + w * short * BF16
+    got = out.gather(1, at)[:, 0]
+    within(got, -w * short, bound)
+    within(loss, -torch.log1p(-short), depth * FP32 + short * 2.0 ** -14)
