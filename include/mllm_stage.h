@@ -451,7 +451,7 @@ mllm_status_t mllm_op_qk_norm_rope_bwd(const void* dy, const void* x, const void
  *   vocab on 0; rows dlogits_stride apart; NULL: the loss alone.  dloss fp32 [t], the weight of every row's loss; NULL: 1.
  * dlogits may be logits (bf16, same stride) and must not overlap them otherwise.  The logits of a row with a negative target are not
  * read.  Logits of -inf have probability 0 (a target among them: loss +inf); a row that is all -inf, holds +inf or NaN, or whose target is
- * at or beyond vocab gives NaN. */
+ * at or beyond vocab gives NaN.  A row's results do not depend on the rows beside it. */
 mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* targets, const float* dloss, float* loss,
                            void* dlogits, int64_t t, int32_t vocab, int32_t cols, int64_t logits_stride, int64_t dlogits_stride,
                            float scale, void* hip_stream);

@@ -621,6 +621,8 @@ __device__ __forceinline__ float largest(const Logits8<float>* v) {
 __device__ __forceinline__ float rescale(float from, float to) { return from == -INFINITY ? 0.f : __builtin_amdgcn_exp2f((from - to) * LOG2E); }
 
 // PARTS: grid z workgroups a row, each of which reads all of it for the sums and forms one step's gradient (1: all of it).
+// A row is added up in the same order by all forms that may take it, which its length alone says: a thread's vectors in units that every one of them
+// holds a whole number of, each against the maximum so far.  So its bits do not depend on the rows beside it, nor on what is asked for.
 template <typename E, int GROUP, int NV, bool PAST, bool PARTS>
 __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArgs a) {
   constexpr int BLOCK = GROUP < 256 ? 256 : GROUP, WAVES = GROUP / 64;
@@ -642,7 +644,8 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
   asm volatile("" : "+v"(at));                         // as a vector load: the next scalar one would wait for it
   const E raw = x[at];
   asm volatile("" ::: "memory");                       // requested in front of the row: waited for behind it, it is 0.7 us of a row's 12 (131072 logits)
-  constexpr int STEP = NV * GROUP;
+  constexpr int STEP = NV * GROUP, UNIT = GROUP < 1024 ? NV : sizeof(E) == 2 ? 4 : 2;
+  static_assert(NV % UNIT == 0, "a step holds whole units");
   Logits8<E> v[NV];
   float m = -INFINITY, s = 0.f;
   for (int from = (nvec - 1) / STEP * STEP; from >= 0; from -= STEP) {   // the first vectors last: they are what stays
@@ -656,23 +659,28 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
 #pragma unroll
       for (int j = 0; j < NV; j++)
         if (from + tid + j * GROUP == nvec - 1) v[j].keep(tail);
-    const float n = fmaxf(m, largest<NV>(v));
-    s *= rescale(m, n);
-    m = n;
-    const float c = m == -INFINITY ? 0.f : m;          // nothing but -inf: s is 0 of no weight
 #pragma unroll
-    for (int j = 0; j < NV; j++) {
-      v[j].settle();
-      float f[8];
-      v[j].get(f);
+    for (int u = NV - UNIT; u >= 0; u -= UNIT) {
+      const float n = fmaxf(m, largest<UNIT>(v + u)), before = rescale(m, n);
+      m = n;
+      const float c = m == -INFINITY ? 0.f : m;        // nothing but -inf: s is 0 of no weight
 #pragma unroll
-      for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f((f[e] - c) * LOG2E);
-      s += ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+      for (int j = u; j < u + UNIT; j++) {
+        v[j].settle();
+        float f[8];
+        v[j].get(f);
+#pragma unroll
+        for (int e = 0; e < 8; e++) f[e] = __builtin_amdgcn_exp2f((f[e] - c) * LOG2E);
+        const float sum = ((f[0] + f[1]) + (f[2] + f[3])) + ((f[4] + f[5]) + (f[6] + f[7]));
+        s = j == u ? fmaf(s, before, sum) : s + sum;     // written out, as below: which products it fuses the compiler decides for each form
+      }
     }
   }
   // all threads' (m, s) in one (without anything but -inf s ends as 0, and the differences of m below as NaN)
   float top = over_lanes<64, true>(m);
-  s = over_lanes<64, false>(s * rescale(m, top));
+  s *= rescale(m, top);
+  asm("" : "+v"(s));
+  s = over_lanes<64, false>(s);
   if (WAVES > 1) {
     if ((threadIdx.x & 63) == 0) wave_sums[threadIdx.x >> 6] = make_float2(top, s);
     __syncthreads();
@@ -683,7 +691,7 @@ __global__ __launch_bounds__(GROUP < 256 ? 256 : GROUP) void xent_kernel(XentArg
     top = most;
     s = 0.f;
 #pragma unroll
-    for (int i = 0; i < WAVES; i++) s += w[i].y * rescale(w[i].x, top);
+    for (int i = 0; i < WAVES; i++) s = fmaf(w[i].y, rescale(w[i].x, top), s);
   }
   const float xt = target < a.vocab ? value(raw) : __uint_as_float(0x7fc00000u);
   if (tid == 0 && part == 0) a.loss[row] = (float)((double)log2f(s) * (1.0 / (double)LOG2E) + ((double)top - (double)xt));
@@ -920,13 +928,18 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   // 131072 1024x20 4.8, 512x16 4.6; 256000 1024x20 4.7.  fp32: 1000 64x2 5.9; 4096 256x4 5.9; 16384 512x8 6.1, 1024x8 4.6; 65536 1024x10 5.3,
   // 512x8 4.8; 131072 1024x10 4.6, 512x16 4.3.
   // Few long rows: as many workgroups a row as it has steps, while every one has a CU to itself.  A lone workgroup is bound by its own exponentials,
-  // two a logit, of which this spares it most of the second (131072 logits, one row 18.0 -> 14.2 us, fp32 17.7 -> 11.5, 64 rows 21.5 -> 17.3;
-  // 260000, 64 rows 37.4 -> 25.7).  Not over the logits themselves, which the other workgroups of the row still read.
+  // two a logit, of which this spares it most of the second (131072 logits, one row 18.0 -> 14.2 us, fp32 17.7 -> 11.9, 64 rows 21.5 -> 17.2;
+  // 260000, 64 rows 37.4 -> 25.9).  Not over the logits themselves, which the other workgroups of the row still read: in place the shorter steps
+  // alone are worth 18.3 us for 18.7, 64 rows 21.3 for 21.8, 32 rows of 196608 28.3 for 34.1.
+  // The loss alone has nothing to hold a row for, and with few vectors a thread twice the workgroups a CU, whatever the rows: 8192 x 131072 350 us for
+  // 410, 300 rows 23.7 for 28.4, fp32 2999 x 50257 105 for 111, 1000 x 131072 95 for 104.  (3000 x 70000 113 for 82: those keep 512x16.)
   const int64_t parts = ceil_div(nvec, logits_fp32 ? 4 * 1024 : 8 * 1024);
-  if (parts > 1 && a.t * parts <= 256) {
+  if (parts > 1 && (a.t * parts <= 256 || (!a.dlogits && (logits_fp32 || nvec > 12288)))) {
     if (a.dlogits && a.dlogits != a.logits) grid.z = (unsigned)parts;
     if (logits_fp32)
       hipLaunchKernelGGL((xent_kernel<float, 1024, 4, false, true>), grid, dim3(1024), 0, s, a);
+    else if (nvec <= 12288)
+      hipLaunchKernelGGL((xent_kernel<bf16_t, 512, 16, false, true>), grid, dim3(512), 0, s, a);
     else
       hipLaunchKernelGGL((xent_kernel<bf16_t, 1024, 8, false, true>), grid, dim3(1024), 0, s, a);
   } else if (logits_fp32) {

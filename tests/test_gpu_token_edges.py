@@ -68,3 +68,31 @@ def test_target_s_gradient_of_confident_rows(B, t, vocab, fp32):
     got = out.gather(1, at)[:, 0]
     within(got, -w * short, bound)
     within(loss, -torch.log1p(-short), depth * FP32 + short * 2.0 ** -14)
+
+
+@pytest.mark.parametrize("fp32", [0, 1])
+@pytest.mark.parametrize("vocab,cols", [(1000, 1000), (32771, 32784), (50257, 50264), (65544, 65544), (98301, 98304), (98309, 98312), (131072, 131072),
+                                        (163841, 163848), (200003, 200016), (262145, 262152)])
+def test_a_row_s_loss_and_gradient_do_not_depend_on_the_rows_beside_it(B, vocab, cols, fp32):
+    """Alone, among a few and among many, with the gradient, without it and in place: the same bits."""
+    t, g = 300, gen(vocab)
+    logits = randn(g, t, cols, scale=4.0, dtype=torch.float32 if fp32 else torch.bfloat16)
+    targets = torch.randint(-1, vocab, (t,), generator=g, device="cuda", dtype=torch.int32)
+    targets[:4] = vocab - 1 - torch.arange(4, device="cuda", dtype=torch.int32)
+    weights = torch.rand(t, generator=g, device="cuda") + 0.5
+
+    def call(rows, grad=True, place=False):
+        x = logits[rows].clone()
+        loss = torch.full((len(x),), float("nan"), device="cuda")
+        out = None if not grad else x if place else torch.full((len(x), cols), 7.0, dtype=torch.bfloat16, device="cuda")
+        B.mllm_op_xent(x, targets[rows], loss, out, len(x), vocab, cols, dloss=weights[rows], scale=0.37, logits_fp32=fp32)
+        return loss, out
+
+    loss, out = call(slice(0, t))
+    for rows in (slice(0, 1), slice(3, 4), slice(0, 2), slice(0, 7), slice(0, 30), slice(0, 64), slice(0, 65), slice(0, 129), slice(200, 300)):
+        few, part = call(rows)
+        assert torch.equal(few, loss[rows]) and torch.equal(part, out[rows]), rows
+        assert torch.equal(call(rows, grad=False)[0], loss[rows]), rows
+        if not fp32:
+            few, part = call(rows, place=True)
+            assert torch.equal(few, loss[rows]) and torch.equal(part, out[rows]), rows
