@@ -82,6 +82,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ ta
     const int32_t id = ids[row];
     const float nothing = id < 0 ? 0.f : __uint_as_float(0x7fc00000u);
     const bool there = id >= 0 && id < vocab;
+    const float by = there ? scale : 1.f;                  // a scale that is no number leaves them zero
     const E* src = table + (there ? (int64_t)id * nvec * 8 : 0);
     float v[EMBED_VECS][8];
 #pragma unroll
@@ -95,7 +96,7 @@ __global__ __launch_bounds__(256) void embed_fwd_kernel(const E* __restrict__ ta
     for (int j = 0; j < EMBED_VECS; j++) {
       const int c = c0 + j * LPR;
 #pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] *= scale;
+      for (int e = 0; e < 8; e++) v[j][e] *= by;
       if (c < nvec) store16<PAST>(y + row * ldy + (int64_t)c * 8, pack8(v[j]));
     }
   }

@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, gen, randn, within  # noqa: E402
+from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, gen, randn, within  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -14,6 +14,24 @@ def B():
     from paper_2603_25120_amd import binding
     binding.lib()
     return binding
+
+
+# ---------------------------------------------------------------------------------------------
+# embedding
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("scale", [0.0, -2.0, float("inf"), float("nan")])
+@pytest.mark.parametrize("fp32", [0, 1])
+def test_rows_without_a_token_are_zero_whatever_the_scale(B, fp32, scale):
+    g = gen(3)
+    t, vocab, d = 70, 50, 264
+    table, ids = randn(g, vocab, d, dtype=torch.float32 if fp32 else torch.bfloat16), draw_ids("mixed", t, vocab, g)
+    y = torch.full((t, d), 7.0, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_embed_fwd(table, ids, y, t, vocab, d, scale=scale, table_fp32=fp32)
+    want = table.double()[ids.clamp(0, vocab - 1).long()] * scale
+    want[ids < 0], want[ids >= vocab] = 0.0, float("nan")
+    assert bool((ids < 0).any()) and bool((ids >= vocab).any())
+    within(y, want, want.abs() * (BF16 + FP32))
+    assert not bool(y[ids < 0].view(torch.int16).any())      # +0
 
 
 # ---------------------------------------------------------------------------------------------
