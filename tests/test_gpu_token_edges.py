@@ -54,6 +54,19 @@ def test_one_gradient_for_both_gains(B, t, hq, hkv, hd, rotate):
     within(both, 2 * want, 2 * bound + 4 * (sums[0].abs() + sums[1].abs()) * FP32)      # two more additions
 
 
+def test_positions_outside_the_table_make_their_gradients_nan(B):
+    """dx of those rows, and the gains' gradients, which take terms of every row; the other rows of dx as they were."""
+    p = Heads(B, 40, 3, 1, 64, True)
+    good, dx, gq, gk = torch.empty_like(p.x), torch.empty_like(p.x), torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
+    p.bwd(p.dy, p.x, good, gq, gk)
+    bad = torch.zeros(40, dtype=torch.bool, device="cuda")
+    for row, v in ((0, -1), (7, p.n_pos), (39, (1 << 31) - 1)):
+        p.pos[row], bad[row] = v, True
+    p.bwd(p.dy, p.x, dx, gq, gk)
+    assert bool(dx[bad][:, :p.width].isnan().all()) and torch.equal(dx[~bad][:, :p.width], good[~bad][:, :p.width])
+    assert bool(gq.isnan().all()) and bool(gk.isnan().all())
+
+
 # ---------------------------------------------------------------------------------------------
 # loss
 # ---------------------------------------------------------------------------------------------
