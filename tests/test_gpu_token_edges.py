@@ -6,7 +6,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, gen, randn, within  # noqa: E402
+from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, garbage, gen, randn, within  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -32,6 +32,24 @@ def test_rows_without_a_token_are_zero_whatever_the_scale(B, fp32, scale):
     assert bool((ids < 0).any()) and bool((ids >= vocab).any())
     within(y, want, want.abs() * (BF16 + FP32))
     assert not bool(y[ids < 0].view(torch.int16).any())      # +0
+
+
+@pytest.mark.parametrize("accumulate", [0, 1])
+@pytest.mark.parametrize("t,vocab,d,how", [(30000, 500, 136, "one"), (30000, 500, 136, "two"), (100000, 3000, 72, "zipf"), (65, 3, 8, "two"),
+                                           (20000, 700, 4096, "one"), (20000, 700, 4096, "two"), (20000, 700, 4096, "zipf"), (16385, 5000, 4096, "uniform"),
+                                           (40000, 700, 4096, "one"), (40000, 700, 4096, "two"), (40000, 700, 4096, "zipf"), (33000, 5000, 4104, "mixed"),
+                                           (64, 7, 520, "one"), (64, 7, 520, "two"), (2999, 50257, 264, "zipf")])
+def test_sums_of_whole_numbers_are_exact(B, t, vocab, d, how, accumulate):
+    """No rounding in any order, so that one row too many or too few shows: chunks of 8, 16 and 32 tokens, ids of a whole microbatch."""
+    g = gen(t + d)
+    ids = draw_ids(how, t, vocab, g)
+    dy = (torch.randint(1, 5, (t, d), generator=g, device="cuda") * (2 * torch.randint(0, 2, (t, d), generator=g, device="cuda") - 1)).bfloat16()
+    before = torch.randint(-9, 10, (vocab, d), generator=g, device="cuda").float()
+    got = before.clone() if accumulate else torch.full_like(before, float("nan"))
+    B.mllm_op_embed_bwd(dy, ids, got, t, vocab, d, garbage(B.mllm_op_embed_bwd_workspace_bytes(t, vocab, d)), scale=-2.0, accumulate=accumulate)
+    held = (ids >= 0) & (ids < vocab)
+    want = torch.zeros(vocab, d, dtype=torch.float64, device="cuda").index_add_(0, ids[held].long(), dy[held].double()) * -2.0
+    assert torch.equal(got.double(), want + before.double() if accumulate else want)
 
 
 # ---------------------------------------------------------------------------------------------
