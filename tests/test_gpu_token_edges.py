@@ -72,6 +72,32 @@ def test_one_gradient_for_both_gains(B, t, hq, hkv, hd, rotate):
     within(both, 2 * want, 2 * bound + 4 * (sums[0].abs() + sums[1].abs()) * FP32)      # two more additions
 
 
+def quarter_turns(n_pos, hd, g):
+    """A table of rotations by 0, 90, 180 and 270 degrees, an angle of its own for every pair."""
+    turn = torch.randint(0, 4, (n_pos, hd // 2), generator=g, device="cuda")
+    return torch.cat([torch.tensor([1.0, 0.0, -1.0, 0.0], device="cuda")[turn], torch.tensor([0.0, 1.0, 0.0, -1.0], device="cuda")[turn]], 1).contiguous()
+
+
+@pytest.mark.parametrize("rotate", [False, True])
+@pytest.mark.parametrize("t,hq,hkv,hd", [(1, 1, 1, 16), (9000, 14, 2, 64), (1500, 28, 4, 128), (33000, 32, 8, 128), (8000, 12, 3, 256), (4097, 7, 1, 32),
+                                         (70001, 4, 4, 16), (777, 32, 8, 128), (20000, 1, 3, 64)])
+def test_gains_gradients_of_whole_numbers_are_exact(B, t, hq, hkv, hd, rotate):
+    """Heads of +1 and -1 keep their values in the norm (eps 0), and whole numbers in dy make whole terms: one head too many or too few
+    shows, in lane groups that walk over many heads as well."""
+    p = Heads(B, t, hq, hkv, hd, rotate)
+    g, p.eps = gen(hd), 0.0
+    p.x = (2 * torch.randint(0, 2, p.x.shape, generator=g, device="cuda") - 1).bfloat16()
+    p.dy = (torch.randint(1, 5, p.dy.shape, generator=g, device="cuda") * (2 * torch.randint(0, 2, p.dy.shape, generator=g, device="cuda") - 1)).bfloat16()
+    if rotate:
+        p.table = quarter_turns(p.n_pos, hd, g)
+    _, _, sums, _ = p.want_bwd()
+    dx, q, k = torch.empty_like(p.x), *(torch.full((hd,), float("nan"), device="cuda") for _ in range(2))
+    p.bwd(p.dy, p.x, dx, q, k)
+    assert torch.equal(q.double(), sums[0]) and torch.equal(k.double(), sums[1])
+    p.bwd(p.dy, p.x, dx, q, k, accumulate=1)
+    assert torch.equal(q.double(), 2 * sums[0]) and torch.equal(k.double(), 2 * sums[1])
+
+
 def test_positions_outside_the_table_make_their_gradients_nan(B):
     """dx of those rows, and the gains' gradients, which take terms of every row; the other rows of dx as they were."""
     p = Heads(B, 40, 3, 1, 64, True)
