@@ -3,9 +3,12 @@ import math
 
 import pytest
 
+import workloads as W
+
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
+from tests.gpu_util import GpuStage  # noqa: E402
 from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, garbage, gen, randn, within  # noqa: E402
 
 
@@ -171,3 +174,22 @@ def test_a_row_s_loss_and_gradient_do_not_depend_on_the_rows_beside_it(B, vocab,
         if not fp32:
             few, part = call(rows, place=True)
             assert torch.equal(few, loss[rows]) and torch.equal(part, out[rows]), rows
+
+
+# ---------------------------------------------------------------------------------------------
+# stages
+# ---------------------------------------------------------------------------------------------
+@pytest.mark.parametrize("seed", [5, 2, 3, 11])
+def test_a_sample_of_a_headnorm_stage_does_not_depend_on_what_is_packed_with_it(B, seed):
+    wl = W.workload_tiny_headnorm(seed)
+    st = GpuStage(B, wl.layers)
+    try:
+        y, dx_img, dx_seq, _ = st.run(wl)
+        cu = wl.batch.seq.cu_seqlens
+        for s, sample in enumerate(wl.batch.samples):
+            img, seq = slice(64 * s, 64 * (s + 1)), slice(cu[s], cu[s + 1])
+            one = W.Workload("one", wl.layers, W.batch_from_samples([sample], img_tokens=64), wl.params, wl.x_img[img], wl.x_seq[seq], wl.dy[seq])
+            y1, dx_img1, dx_seq1, _ = st.run(one)
+            assert torch.equal(y1, y[seq]) and torch.equal(dx_img1, dx_img[img]) and torch.equal(dx_seq1, dx_seq[seq])
+    finally:
+        st.close()
