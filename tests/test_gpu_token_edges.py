@@ -9,7 +9,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from tests.gpu_util import GpuStage  # noqa: E402
-from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, garbage, gen, randn, within  # noqa: E402
+from tests.test_gpu_token_ops import BF16, FP32, SHAPES, Heads, draw_ids, garbage, gen, randn, want_loss, within  # noqa: E402
 
 
 @pytest.fixture(scope="module")
@@ -174,6 +174,32 @@ def test_a_row_s_loss_and_gradient_do_not_depend_on_the_rows_beside_it(B, vocab,
         if not fp32:
             few, part = call(rows, place=True)
             assert torch.equal(few, loss[rows]) and torch.equal(part, out[rows]), rows
+
+
+@pytest.mark.parametrize("fp32", [0, 1])
+@pytest.mark.parametrize("vocab,cols", [(50257, 50264), (70001, 70008), (131072, 131072), (200003, 200016)])
+def test_masked_and_broken_rows_among_many(B, vocab, cols, fp32):
+    """The forms for many long rows, on rows that hold no number or none but masked ones."""
+    inf, nan, t, g = float("inf"), float("nan"), 300, gen(vocab)
+    kind = torch.float32 if fp32 else torch.bfloat16
+    logits, low = randn(g, t, cols, dtype=kind), torch.finfo(kind).min
+    targets = torch.randint(0, 40, (t,), generator=g, device="cuda", dtype=torch.int32)
+    for base in (0, 137, 290):
+        logits[base, 45:], logits[base + 1, 45:], logits[base + 2, int(targets[base + 2])] = -inf, low, -inf
+        logits[base + 3], logits[base + 4, 41], logits[base + 5, vocab - 1] = -inf, inf, nan
+        targets[base + 6], targets[base + 7] = vocab, -1
+        logits[base + 8], logits[base + 9] = low, -inf
+        logits[base + 9, int(targets[base + 9])] = 3.0
+    logits[:, vocab:] = nan
+    loss, out = torch.empty(t, device="cuda"), torch.empty(t, cols, dtype=torch.bfloat16, device="cuda")
+    B.mllm_op_xent(logits, targets, loss, out, t, vocab, cols, logits_fp32=fp32)
+    for rows in torch.arange(t, device="cuda").split(50):
+        want, size, grad, bound = want_loss(logits[rows], targets[rows], vocab, 1.0, None)
+        within(loss[rows], want, size, "loss")
+        within(out[rows], grad, bound, "gradient")
+    alone = torch.empty(t, device="cuda")
+    B.mllm_op_xent(logits, targets, alone, None, t, vocab, cols, logits_fp32=fp32)
+    assert torch.equal(alone.view(torch.int32)[~loss.isnan()], loss.view(torch.int32)[~loss.isnan()]) and torch.equal(alone.isnan(), loss.isnan())
 
 
 # ---------------------------------------------------------------------------------------------
