@@ -432,7 +432,7 @@ mllm_status_t mllm_op_qk_norm_rope_fwd(const void* x, const void* gamma_q, const
                                        const float* rope_table, int64_t n_pos, int64_t t, int32_t n_q_heads, int32_t n_kv_heads,
                                        int32_t head_dim, int64_t x_stride, int64_t y_stride, float eps, void* hip_stream);
 /* Its gradients, from dy (the gradient of y) and the x that entered: dx in the same columns (rows dx_stride apart; dx may be dy or
- * x with the same stride), dgamma_q and dgamma_k fp32 [head_dim] (accumulate != 0: +=).  Queries and keys that
+ * x with the same stride and must not overlap them otherwise), dgamma_q and dgamma_k fp32 [head_dim] (accumulate != 0: +=).  Queries and keys that
  * have one gain may have one gradient, which then takes the sum of both (two launches more); otherwise the two must not overlap.  A position
  * outside [0, n_pos) makes its row of dx NaN and with it the gains' gradients, which take terms of every row.  With the
  * gradient of the rotation already taken (mllm_op_attn_bwd_rope) pass no rope_table.  partial: fp32 scratch of

@@ -550,7 +550,8 @@ __global__ __launch_bounds__(QK_THREADS) void qk_norm_bwd_kernel(QkNormArgs a, f
 // Loss over the vocabulary and its gradient, the row read once: GROUP threads hold up to NV vectors of eight logits each in registers
 // from the maximum to the gradient; of a longer row the vectors behind the first GROUP * NV are read again for the gradient.  With the
 // maximum m and L = log2(e):  s = sum 2^((x - m) L), loss = log2(s) / L + (m - x[target]), gradient = 2^((x - m) L - log2(s) + log2 |weight|)
-// with the weight's sign, and |weight| (2^((x - m) L) / s - 1) at the target.  Every thread sums against its own maximum, so that one exchange joins (m, s) of all.
+// with the weight's sign, and |weight| (2^((x - m) L) / s - 1) at the target.  Every thread sums against its own maximum, so that one exchange
+// joins (m, s) of all.
 // (x L - m L in one instruction would lose rows of the type's lowest value: m L is beyond the largest number.)
 // ---------------------------------------------------------------------------------------------
 constexpr float LOG2E = 1.4426950408889634f;
@@ -570,7 +571,7 @@ struct Logits8<bf16_t> {
   __device__ __forceinline__ void load(const bf16_t* p) { u = *reinterpret_cast<const u32x4*>(p); }
   __device__ __forceinline__ void none() { u = 0xff80ff80u; }   // -inf
   __device__ __forceinline__ void get(float* f) const { unpack8(make_uint4(u[0], u[1], u[2], u[3]), f); }
-  // Keeps the compiler from carrying the unpacked values from one use to the next (129 registers spilled with 16 vectors).
+  // Keeps the compiler from carrying unpacked values from one use to the next (16384 x 32000: 339 us, 343 without).
   __device__ __forceinline__ void settle() { asm volatile("" : "+v"(u)); }
   __device__ __forceinline__ void keep(int n) {   // the first n, 1 to 7
 #pragma unroll
@@ -924,16 +925,15 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
     else hipLaunchKernelGGL((xent_kernel<E, GROUP, NV, false, false>), grid, dim3(GROUP < 256 ? 256 : GROUP), 0, s, a);     \
   } while (0)
   // Threads times vectors that hold a row with the least idle and two workgroups a CU at least where that goes; TB/s of what a pass
-  // reads and writes, rows of bf16: 1000 columns 64x2 5.1, 64x4 4.2; 4096 256x2 5.4, 256x4 4.6; 8192 256x4 5.8, 512x4 5.1; 16384 512x4 5.9,
-  // 256x8 5.5; 24000 512x8 5.8, 1024x4 5.2; 27000 and 32000 1024x4 5.9 and 6.1, 512x8 5.5 and 5.6; 65536 512x16 5.4, 1024x8 4.9; 96000 (a third of the row read again) 512x16 5.1, 1024x20 4.4;
-  // 131072 1024x20 4.8, 512x16 4.6; 256000 1024x20 4.7.  fp32: 1000 64x2 5.9; 4096 256x4 5.9; 16384 512x8 6.1, 1024x8 4.6; 65536 1024x10 5.3,
-  // 512x8 4.8; 131072 1024x10 4.6, 512x16 4.3.
+  // reads and writes, rows of bf16: 1000 columns 64x2 5.7, 64x4 4.4; 2000 64x4 6.6, 256x2 3.7; 4096 256x2 5.7, 256x4 4.9; 8192 256x4 5.8, 512x4 5.0;
+  // 16384 512x4 5.4, 256x8 5.5; 24000 512x8 5.6, 1024x4 5.7; 27000 and 32000 1024x4 5.7 and 6.2, 512x8 5.2 and 5.5; 65536 512x16 5.5, 1024x8 5.1; 96000 (a third
+  // of the row read again) 512x16 5.3, 1024x20 4.7; 131072 1024x20 5.1, 512x16 4.9; 256000 1024x20 4.7.  fp32: 1000 64x2 5.8; 4096 256x4 5.9; 16384
+  // 512x8 6.2, 1024x8 3.7; 65536 1024x10 5.4, 512x8 5.2; 131072 1024x10 4.7, 512x16 4.6.
   // Few long rows: as many workgroups a row as it has steps, while every one has a CU to itself.  A lone workgroup is bound by its own exponentials,
   // two a logit, of which this spares it most of the second (131072 logits, one row 18.0 -> 14.2 us, fp32 17.7 -> 11.9, 64 rows 21.5 -> 17.2;
   // 260000, 64 rows 37.4 -> 25.9).  Not over the logits themselves, which the other workgroups of the row still read: in place the shorter steps
   // alone are worth 18.3 us for 18.7, 64 rows 21.3 for 21.8, 32 rows of 196608 28.3 for 34.1.
-  // The loss alone has nothing to hold a row for, and with few vectors a thread twice the workgroups a CU, whatever the rows: 8192 x 131072 350 us for
-  // 410, 300 rows 23.7 for 28.4, fp32 2999 x 50257 105 for 111, 1000 x 131072 95 for 104.  (3000 x 70000 113 for 82: those keep 512x16.)
+  // The loss alone has nothing to hold a row for and takes shorter steps for any number of rows: 8192 x 131072 350 us for 410, 300 rows 23.7 for 28.4, fp32 2999 x 50257 105 for 111, 1000 x 131072 95 for 104.  (3000 x 70000 113 for 82: those keep 512x16.)
   const int64_t parts = ceil_div(nvec, logits_fp32 ? 4 * 1024 : 8 * 1024);
   if (parts > 1 && (a.t * parts <= 256 || (!a.dlogits && (logits_fp32 || nvec > 12288)))) {
     if (a.dlogits && a.dlogits != a.logits) grid.z = (unsigned)parts;
