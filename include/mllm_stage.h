@@ -414,7 +414,8 @@ mllm_status_t mllm_op_embed_fwd(const void* table, int table_fp32, const int32_t
 /* The table's gradient: dtable [vocab, d] fp32 = scale * (sum of the rows of dy whose id it is), added up in an order that the ids fix;
  * accumulate != 0: added to what dtable holds, rows of other ids untouched.  dy bf16 [t, d], rows dy_stride apart.  Ids outside
  * [0, vocab) contribute nothing.  workspace: mllm_op_embed_bwd_workspace_bytes, 256-byte aligned, contents undefined afterwards (the
- * token lists by id and partial sums; the same bytes serve fewer tokens with the same vocab and d). */
+ * token lists by id and partial sums; the same bytes serve fewer tokens with the same vocab and d).  More than 64 tokens are sorted by
+ * id, every id read once or twice for each 1024 ids of the table. */
 size_t mllm_op_embed_bwd_workspace_bytes(int64_t t, int64_t vocab, int64_t d);
 mllm_status_t mllm_op_embed_bwd(const void* dy, const int32_t* ids, float* dtable, int accumulate, int64_t t, int64_t vocab,
                                 int64_t d, int64_t dy_stride, float scale, void* workspace, size_t workspace_bytes,

@@ -933,7 +933,8 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s) {
   // two a logit, of which this spares it most of the second (131072 logits, one row 18.0 -> 14.2 us, fp32 17.7 -> 11.9, 64 rows 21.5 -> 17.2;
   // 260000, 64 rows 37.4 -> 25.9).  Not over the logits themselves, which the other workgroups of the row still read: in place the shorter steps
   // alone are worth 18.3 us for 18.7, 64 rows 21.3 for 21.8, 32 rows of 196608 28.3 for 34.1.
-  // The loss alone has nothing to hold a row for and takes shorter steps for any number of rows: 8192 x 131072 350 us for 410, 300 rows 23.7 for 28.4, fp32 2999 x 50257 105 for 111, 1000 x 131072 95 for 104.  (3000 x 70000 113 for 82: those keep 512x16.)
+  // The loss alone has nothing to hold a row for and takes shorter steps for any number of rows: 8192 x 131072 350 us for 410, 300 rows 23.7 for 28.4,
+  // fp32 2999 x 50257 105 for 111, 1000 x 131072 95 for 104.  (3000 x 70000 113 for 82: those keep 512x16.)
   const int64_t parts = ceil_div(nvec, logits_fp32 ? 4 * 1024 : 8 * 1024);
   if (parts > 1 && (a.t * parts <= 256 || (!a.dlogits && (logits_fp32 || nvec > 12288)))) {
     if (a.dlogits && a.dlogits != a.logits) grid.z = (unsigned)parts;
