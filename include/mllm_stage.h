@@ -459,6 +459,107 @@ mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* t
                            float scale, void* hip_stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Around a layer's products and attention: positions on several axes, the residual stream between two blocks, activations kept in 8 bits.
+ * bf16 and fp32 matrices and vectors start on 16 bytes (MLLM_ERR_UNSUPPORTED otherwise), strides are in elements and multiples of 8.  None of these calls
+ * copies from the host (what they take from there travels with the launch), so all may be captured into a graph; calls that overlap in
+ * time need outputs and scratch of their own.  Sums, statistics and angles' factors are fp32 and each bf16 result is rounded once; same
+ * inputs, same bits.
+ * ------------------------------------------------------------------------------------------ */
+
+/* Positions of a packed sequence on the axes time, height and width: pos device int32 [3][pos_stride], of which the first
+ * cu_seqlens_host[n_segments] entries of every axis are written.  Inside a segment a counter p begins at 0.  A row of text has p on all three axes and takes
+ * one step.  A grid (an image, or the frames of a clip), grids_host [n_grids][5] = first row, frames, height, width, time step of a frame, covers
+ * frames * height * width rows: row (i, j, k) of it has the positions p + i * step, p + j, p + k, and it takes
+ * max((frames - 1) * step + 1, height, width) steps.  Grids are in ascending order of their rows and each lies inside one segment
+ * (MLLM_ERR_INDEX); sizes are positive, steps not negative (MLLM_ERR_SHAPE).  Any number of grids: up to 192 runs of text or grids go into a launch. */
+mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host,
+                                     int32_t* pos, int64_t pos_stride, void* hip_stream);
+/* One more than the largest of these positions: the rows that a table of rotary factors needs (host only, 0 without rows). */
+mllm_status_t mllm_grid_positions_count(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host,
+                                        int64_t* n_pos);
+/* Rotary factors for any list of frequencies (frequencies_host: n_pairs numbers, radians a position): table device fp32
+ * [n_pos, 2 n_pairs], row p the cosines of p * frequency, then the sines; angles and their sines in fp64.  n_pairs at most 128.  With
+ * rope_base^(-2i/head_dim) for i < head_dim/2 it is the table of mllm_op_rope_table. */
+mllm_status_t mllm_op_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const double* frequencies_host, void* hip_stream);
+/* Rotation of heads whose pairs follow several axes.  x bf16 [t, x_stride], the leading n_heads heads of head_dim columns of a row; pair i < n_pairs of
+ * a head, its elements i and i + n_pairs, is turned by the angle of table row pos[pair_axis_host[i]][row] (pos device int32
+ * [n_axes][pos_stride]; n_axes at most 4), inverse != 0: by the negative angle, which is the gradient; elements from 2 n_pairs on stay as
+ * they are.  table: device fp32 [n_pos, 2 n_pairs] from mllm_op_rope_freq_table or mllm_op_rope_table.  A position outside [0, n_pos) reads
+ * nothing and makes the row's pairs of that axis NaN.  y receives the same columns, other columns are not touched; y may be x with the same
+ * stride and must not overlap it otherwise.  head_dim: a multiple of 8, at most 256; n_pairs: a positive multiple of 8, at most head_dim / 2; n_heads: at
+ * most 65535. */
+mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int64_t pos_stride, int32_t n_axes,
+                                const uint8_t* pair_axis_host, int32_t n_pairs, const float* table, int64_t n_pos, int64_t t,
+                                int32_t n_heads, int32_t head_dim, int64_t x_stride, int64_t y_stride, int inverse, void* hip_stream);
+
+/* The residual stream between two blocks in one pass: x bf16 [t, d] the stream, o bf16 [t, d] the output of a block,
+ *   u = post(o) * scale * g     y = x + u (bf16)     n = pre(y), of y as it is stored
+ * post and pre: MLLM_NORM_LAYER with gain and shift, MLLM_NORM_RMS with gain, or MLLM_NORM_NONE; scale [d] or NULL (1); g = gate_act(gate),
+ * gate fp32: one value for the block, or (gate_per_row) one for every row (dropped samples have 0), or NULL (1). */
+enum { MLLM_NORM_LAYER = 0, MLLM_NORM_RMS = 1, MLLM_NORM_NONE = 2 };
+enum { MLLM_GATE_LINEAR = 0, MLLM_GATE_TANH = 1, MLLM_GATE_SIGMOID = 2 };
+typedef struct {
+  int32_t post_kind, pre_kind;   /* MLLM_NORM_*                                                        */
+  int32_t gate_act;              /* MLLM_GATE_*                                                        */
+  int32_t gate_per_row;          /* gate holds t values instead of one                                 */
+  float post_eps, pre_eps;
+  const void* post_g;            /* device bf16 [d] each; those that the kinds do not name are ignored */
+  const void* post_b;
+  const void* scale;
+  const void* pre_g;
+  const void* pre_b;
+  const float* gate;             /* device fp32 [1] or [t]                                             */
+} mllm_residual_norm_t;
+/* The parameters' gradients, device fp32 of the parameters' sizes; NULL: not wanted. */
+typedef struct {
+  float* post_g;
+  float* post_b;
+  float* scale;
+  float* pre_g;
+  float* pre_b;
+  float* gate;
+} mllm_residual_norm_grads_t;
+/* Forward.  n: ignored with pre MLLM_NORM_NONE.  stats fp32 [4, t] for the backward pass: factor and mean of post, factor and mean of pre (rows of a
+ * kind that has none are left alone).  y may be x; no other output may overlap an input or another output.  d: a multiple of 8, at most 8192. */
+mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const void* x, const void* o, void* y, void* n, float* stats,
+                                        int64_t t, int64_t d, void* hip_stream);
+/* Backward, from the gradients dn of n (ignored with pre MLLM_NORM_NONE) and dy of y (bf16 [t, d]; NULL: none, only with a pre norm), and y, o and stats of
+ * the forward pass: dx of x, d_o of o (bf16 [t, d]) and the parameters' gradients, of which accumulate != 0 adds to what is there, except
+ * the gate's with gate_per_row, which is always overwritten.  dx and d_o may each be dn or dy, and overlap nothing otherwise; the gradients
+ * are different buffers.  partial: fp32 scratch of mllm_op_residual_norm_bwd_partial_bytes (the same bytes serve fewer rows of the same d). */
+size_t mllm_op_residual_norm_bwd_partial_bytes(int64_t t, int64_t d);
+mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const void* dn, const void* dy, const void* y, const void* o,
+                                        const float* stats, void* dx, void* d_o, const mllm_residual_norm_grads_t* grads, int accumulate,
+                                        float* partial, int64_t t, int64_t d, void* hip_stream);
+
+/* Activations kept in 8 bits from the forward to the backward pass: x bf16 [t, width] (width a multiple of 8) becomes q, [t, width] bytes, and exponents,
+ * [t, ceil(width / 32)] bytes, 33/64 of its size.  Every 32 neighbouring columns of a row (the last ones fewer) are a block with an exponent
+ * e, the smallest from -112 on with max |x| <= L * 2^e, and q holds x * 2^-e rounded to the nearest (ties to even) of the format:
+ * MLLM_KEEP_INT8 whole numbers, L = 127; MLLM_KEEP_E4M3 8-bit floating point (OCP E4M3), L = 448.  The exponent's byte is e + 127.  The values
+ * q * 2^e are bf16 numbers, so nothing else is rounded (2^128, to which numbers from 3.28e38 on may be rounded, comes back as an infinity).
+ * A block that holds an infinity or a NaN has the byte 255 and comes back as NaN. */
+enum { MLLM_KEEP_INT8 = 0, MLLM_KEEP_E4M3 = 1 };
+mllm_status_t mllm_op_keep8(const void* x, void* q, void* exponents, int64_t t, int64_t width, int64_t x_stride, int format,
+                            void* hip_stream);
+mllm_status_t mllm_op_keep8_load(const void* q, const void* exponents, void* y, int64_t t, int64_t width, int64_t y_stride, int format,
+                                 void* hip_stream);
+/* mllm_op_act_fwd that keeps what the activation is taken of in 8 bits: pre [t, f], or for SwiGLU [gate | up] [t, 2f], each half in blocks of its own:
+ * q [t, f] or [t, 2f], exponents [t, ceil(f / 32)] or [t, 2 ceil(f / 32)].  a bf16 [t, f] comes from pre itself. */
+mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* exponents, int64_t t, int64_t f, int format,
+                                    void* hip_stream);
+/* mllm_op_act_bwd from there: dpre (like pre) from da [t, f] and the kept values; a [t, f] (or NULL) receives the activation of the kept values, which the
+ * next map's weight gradient takes, so that no activation need be kept.  da and dpre both NULL: the activation alone.  dpre may be da for
+ * the GELU kinds; nothing else may overlap. */
+mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, const void* exponents, void* dpre, void* a, int64_t t,
+                                    int64_t f, int format, void* hip_stream);
+/* mllm_op_linear_bwd with x [t, k] kept in 8 bits by mllm_op_keep8.  workspace: mllm_op_linear_bwd_keep8_workspace_bytes, 256-byte aligned; with
+ * less a product may be cut into fewer parts, below 2 t k bytes (rounded up to 256) the call is refused. */
+size_t mllm_op_linear_bwd_keep8_workspace_bytes(int64_t t, int64_t k, int64_t n);
+mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void* exponents, const void* w, void* dx, void* dw, int64_t t,
+                                       int64_t k, int64_t n, int format, int accumulate, void* workspace, size_t workspace_bytes,
+                                       void* hip_stream);
+
+/* ------------------------------------------------------------------------------------------
  * Online microbatch scheduler (host only, no GPU work; Online Microbatch Scheduler, "Problem
  * Formulation" and "Scheduling Optimization").  Item i of a global batch has an encoder-stage
  * duration e_dur[i] and an LLM-stage duration l_dur[i] (host arrays, non-negative).  The items are

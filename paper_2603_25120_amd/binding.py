@@ -26,7 +26,10 @@ EXPORTS = ["mllm_stage_create", "mllm_stage_destroy", "mllm_stage_param_count", 
            "mllm_op_norm_bwd_partial_bytes", "mllm_op_norm_bwd", "mllm_op_norm_bwd_colsum", "mllm_op_rope", "mllm_op_rope_table", "mllm_op_gemm_rope", "mllm_op_attn_bwd_rope", "mllm_op_act_fwd",
            "mllm_op_act_bwd", "mllm_op_colsum_partial_bytes", "mllm_op_colsum", "mllm_op_colsum_static_max_bytes", "mllm_op_colsum_static",
            "mllm_op_embed_fwd", "mllm_op_embed_bwd_workspace_bytes", "mllm_op_embed_bwd", "mllm_op_qk_norm_rope_fwd",
-           "mllm_op_qk_norm_rope_bwd_partial_bytes", "mllm_op_qk_norm_rope_bwd", "mllm_op_xent", "mllm_profile_begin",
+           "mllm_op_qk_norm_rope_bwd_partial_bytes", "mllm_op_qk_norm_rope_bwd", "mllm_op_xent", "mllm_op_grid_positions",
+           "mllm_grid_positions_count", "mllm_op_rope_freq_table", "mllm_op_rope_axes", "mllm_op_residual_norm_fwd",
+           "mllm_op_residual_norm_bwd_partial_bytes", "mllm_op_residual_norm_bwd", "mllm_op_keep8", "mllm_op_keep8_load",
+           "mllm_op_act_fwd_keep8", "mllm_op_act_bwd_keep8", "mllm_op_linear_bwd_keep8_workspace_bytes", "mllm_op_linear_bwd_keep8", "mllm_profile_begin",
            "mllm_profile_end", "mllm_schedule_lpt", "mllm_schedule", "mllm_interp", "mllm_item_durations",
            "mllm_find_combs", "mllm_evaluate_parallelism", "mllm_optimize_parallelism"]
 
@@ -71,6 +74,21 @@ class PackC(C.Structure):
 
 class BatchC(C.Structure):
     _fields_ = [("img", PackC), ("seq", PackC), ("img_to_seq_row_host", C.POINTER(C.c_int32))]
+
+
+NORM_LAYER, NORM_RMS, NORM_NONE = 0, 1, 2
+GATE_LINEAR, GATE_TANH, GATE_SIGMOID = 0, 1, 2
+KEEP_INT8, KEEP_E4M3 = 0, 1
+
+
+class ResidualNormC(C.Structure):
+    _fields_ = [("post_kind", C.c_int32), ("pre_kind", C.c_int32), ("gate_act", C.c_int32), ("gate_per_row", C.c_int32),
+                ("post_eps", C.c_float), ("pre_eps", C.c_float), ("post_g", C.c_void_p), ("post_b", C.c_void_p),
+                ("scale", C.c_void_p), ("pre_g", C.c_void_p), ("pre_b", C.c_void_p), ("gate", C.c_void_p)]
+
+
+class ResidualNormGradsC(C.Structure):
+    _fields_ = [(name, C.c_void_p) for name in ("post_g", "post_b", "scale", "pre_g", "pre_b", "gate")]
 
 
 # The same layouts with plain addresses, for the views that a call makes (_PackKeep).
@@ -150,6 +168,21 @@ def lib() -> C.CDLL:
     L.mllm_op_qk_norm_rope_bwd_partial_bytes.restype = sz
     L.mllm_op_qk_norm_rope_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, vp, vp, i64, i64, i32, i32, i32, i64, i64, i64, C.c_float, vp]
     L.mllm_op_xent.argtypes = [vp, C.c_int, vp, vp, vp, vp, i64, i32, i32, i64, i64, C.c_float, vp]
+    L.mllm_op_grid_positions.argtypes = [i32, vp, i32, vp, vp, i64, vp]
+    L.mllm_grid_positions_count.argtypes = [i32, vp, i32, vp, C.POINTER(i64)]
+    L.mllm_op_rope_freq_table.argtypes = [vp, i64, i32, vp, vp]
+    L.mllm_op_rope_axes.argtypes = [vp, vp, vp, i64, i32, vp, i32, vp, i64, i64, i32, i32, i64, i64, C.c_int, vp]
+    L.mllm_op_residual_norm_fwd.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, vp]
+    L.mllm_op_residual_norm_bwd_partial_bytes.argtypes = [i64, i64]
+    L.mllm_op_residual_norm_bwd_partial_bytes.restype = sz
+    L.mllm_op_residual_norm_bwd.argtypes = [vp, vp, vp, vp, vp, vp, vp, vp, vp, C.c_int, vp, i64, i64, vp]
+    L.mllm_op_keep8.argtypes = [vp, vp, vp, i64, i64, i64, C.c_int, vp]
+    L.mllm_op_keep8_load.argtypes = [vp, vp, vp, i64, i64, i64, C.c_int, vp]
+    L.mllm_op_act_fwd_keep8.argtypes = [C.c_int, vp, vp, vp, vp, i64, i64, C.c_int, vp]
+    L.mllm_op_act_bwd_keep8.argtypes = [C.c_int, vp, vp, vp, vp, vp, i64, i64, C.c_int, vp]
+    L.mllm_op_linear_bwd_keep8_workspace_bytes.argtypes = [i64, i64, i64]
+    L.mllm_op_linear_bwd_keep8_workspace_bytes.restype = sz
+    L.mllm_op_linear_bwd_keep8.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, C.c_int, C.c_int, vp, sz, vp]
     L.mllm_profile_begin.argtypes = [i32]
     L.mllm_profile_end.argtypes = [C.POINTER(i64), C.POINTER(C.c_double), C.POINTER(C.c_double), C.POINTER(i64)]
     dp, ip = C.POINTER(C.c_double), C.POINTER(i32)
@@ -483,6 +516,118 @@ def mllm_op_xent(logits, targets, loss, dlogits, t, vocab, cols, logits_stride=N
     _check(lib().mllm_op_xent(_ptr(logits), int(logits_fp32), _ptr(targets), _ptr(dloss), _ptr(loss), _ptr(dlogits), t, vocab, cols,
                               cols if logits_stride is None else logits_stride, cols if dlogits_stride is None else dlogits_stride,
                               scale, _stream(stream)))
+
+
+class PositionGrids:
+    """Samples and grids of a packed microbatch, as mllm_op_grid_positions takes them: cu_seqlens [n + 1]; grids [m, 5] of first row,
+    frames, height, width and a frame's time step."""
+
+    def __init__(self, cu_seqlens, grids=()):
+        self.cu = np.ascontiguousarray(cu_seqlens, dtype=np.int32)
+        self.grids = np.ascontiguousarray(grids, dtype=np.int32).reshape(-1, 5)
+        self.total_tokens = int(self.cu[-1])
+        self.args = (len(self.cu) - 1, _address(self.cu), len(self.grids), _address(self.grids))
+
+
+def mllm_op_grid_positions(grids: PositionGrids, pos, pos_stride=None, stream=None) -> None:
+    """pos: device int32 [3, pos_stride] (pos_stride: the samples' rows, unless it is given)."""
+    _check(lib().mllm_op_grid_positions(*grids.args, _ptr(pos), grids.total_tokens if pos_stride is None else pos_stride, _stream(stream)))
+
+
+def mllm_grid_positions_count(grids: PositionGrids) -> int:
+    n = C.c_int64()
+    _check(lib().mllm_grid_positions_count(*grids.args, C.byref(n)))
+    return int(n.value)
+
+
+def mllm_op_rope_freq_table(table, n_pos, frequencies, stream=None) -> None:
+    f = np.ascontiguousarray(frequencies, dtype=np.float64)
+    _check(lib().mllm_op_rope_freq_table(_ptr(table), n_pos, len(f), _address(f), _stream(stream)))
+
+
+class PairAxes:
+    """The axis that each pair of a head follows."""
+
+    def __init__(self, axes):
+        self.axes = np.ascontiguousarray(axes, dtype=np.uint8)
+        self.n_pairs, self.n_axes, self.address = len(self.axes), int(self.axes.max(initial=0)) + 1, _address(self.axes)
+
+
+def pair_axes(axes) -> PairAxes:
+    return PairAxes(axes)
+
+
+def section_axes(sections, dealt: bool = False) -> PairAxes:
+    """Sections of sections[a] pairs for every axis a, one after the other, or dealt out in turn to the axes that still lack pairs."""
+    if not dealt:
+        return PairAxes([a for a, n in enumerate(sections) for _ in range(n)])
+    return PairAxes([a for i in range(max(sections)) for a, n in enumerate(sections) if i < n])
+
+
+def mllm_op_rope_axes(x, y, pos, axes: PairAxes, table, n_pos, t, n_heads, head_dim, x_stride, y_stride, inverse=0, pos_stride=None,
+                      stream=None) -> None:
+    _check(lib().mllm_op_rope_axes(_ptr(x), _ptr(y), _ptr(pos), t if pos_stride is None else pos_stride, axes.n_axes, axes.address, axes.n_pairs,
+                                   _ptr(table), n_pos, t, n_heads, head_dim, x_stride, y_stride, int(inverse), _stream(stream)))
+
+
+class ResidualNorm:
+    """mllm_residual_norm_t of device tensors, which it keeps."""
+
+    def __init__(self, post_kind=NORM_NONE, post_g=None, post_b=None, post_eps=0.0, scale=None, gate=None, gate_per_row=False,
+                 gate_act=GATE_LINEAR, pre_kind=NORM_NONE, pre_g=None, pre_b=None, pre_eps=0.0):
+        self.tensors = (post_g, post_b, scale, pre_g, pre_b, gate)
+        self.c = ResidualNormC(post_kind, pre_kind, gate_act, int(gate_per_row), post_eps, pre_eps, *[_ptr(v) for v in self.tensors])
+        self.address = C.addressof(self.c)
+
+
+class ResidualNormGrads:
+    """mllm_residual_norm_grads_t of device tensors, which it keeps; None: not wanted."""
+
+    def __init__(self, post_g=None, post_b=None, scale=None, pre_g=None, pre_b=None, gate=None):
+        self.tensors = (post_g, post_b, scale, pre_g, pre_b, gate)
+        self.c = ResidualNormGradsC(*[_ptr(v) for v in self.tensors])
+        self.address = C.addressof(self.c)
+
+
+def mllm_op_residual_norm_fwd(block: ResidualNorm, x, o, y, n, stats, t, d, stream=None) -> None:
+    _check(lib().mllm_op_residual_norm_fwd(block.address, _ptr(x), _ptr(o), _ptr(y), _ptr(n), _ptr(stats), t, d, _stream(stream)))
+
+
+def mllm_op_residual_norm_bwd_partial_bytes(t: int, d: int) -> int:
+    return int(lib().mllm_op_residual_norm_bwd_partial_bytes(t, d))
+
+
+def mllm_op_residual_norm_bwd(block: ResidualNorm, dn, dy, y, o, stats, dx, d_o, grads: ResidualNormGrads, partial, t, d, accumulate=0,
+                              stream=None) -> None:
+    _check(lib().mllm_op_residual_norm_bwd(block.address, _ptr(dn), _ptr(dy), _ptr(y), _ptr(o), _ptr(stats), _ptr(dx), _ptr(d_o),
+                                           grads.address, int(accumulate), _ptr(partial), t, d, _stream(stream)))
+
+
+def mllm_op_keep8(x, q, exponents, t, width, format, x_stride=None, stream=None) -> None:
+    _check(lib().mllm_op_keep8(_ptr(x), _ptr(q), _ptr(exponents), t, width, width if x_stride is None else x_stride, format, _stream(stream)))
+
+
+def mllm_op_keep8_load(q, exponents, y, t, width, format, y_stride=None, stream=None) -> None:
+    _check(lib().mllm_op_keep8_load(_ptr(q), _ptr(exponents), _ptr(y), t, width, width if y_stride is None else y_stride, format, _stream(stream)))
+
+
+def mllm_op_act_fwd_keep8(act, pre, a, q, exponents, t, f, format, stream=None) -> None:
+    _check(lib().mllm_op_act_fwd_keep8(act, _ptr(pre), _ptr(a), _ptr(q), _ptr(exponents), t, f, format, _stream(stream)))
+
+
+def mllm_op_act_bwd_keep8(act, da, q, exponents, dpre, t, f, format, a=None, stream=None) -> None:
+    _check(lib().mllm_op_act_bwd_keep8(act, _ptr(da), _ptr(q), _ptr(exponents), _ptr(dpre), _ptr(a), t, f, format, _stream(stream)))
+
+
+def mllm_op_linear_bwd_keep8_workspace_bytes(t: int, k: int, n: int) -> int:
+    return int(lib().mllm_op_linear_bwd_keep8_workspace_bytes(t, k, n))
+
+
+def mllm_op_linear_bwd_keep8(dy, q, exponents, w, dx, dw, t, k, n, format, workspace, accumulate=0, stream=None, workspace_bytes=None) -> None:
+    if workspace_bytes is None:
+        workspace_bytes = 0 if workspace is None else _nbytes(workspace)
+    _check(lib().mllm_op_linear_bwd_keep8(_ptr(dy), _ptr(q), _ptr(exponents), _ptr(w), _ptr(dx), _ptr(dw), t, k, n, format, int(accumulate),
+                                          _ptr(workspace), workspace_bytes, _stream(stream)))
 
 
 def mllm_profile_begin(max_records: int) -> None:

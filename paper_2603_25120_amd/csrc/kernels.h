@@ -214,6 +214,46 @@ struct XentArgs {
   float scale;
 };
 hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s);
+// Rotary positions with several axes (positions.hip).
+struct PositionRun { int32_t row, position, frame_rows, width, step; };   // a stretch of text (frame_rows 0), or a grid whose frames have that many rows
+constexpr int POSITION_RUNS = 192;                                        // in one launch: they travel as the kernel's argument, which holds 4 KB
+struct PositionRuns { PositionRun run[POSITION_RUNS]; };
+// pos [3][stride]: rows row0 .. row0 + rows of a packed sequence, of which the first run begins at row0 and the last one ends there.
+hipError_t launch_grid_positions(const PositionRuns& runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s);
+constexpr int ROPE_PAIRS = 128, ROPE_AXES = 4;                            // pairs of a head, axes, at most
+struct RopeFrequencies { double frequency[ROPE_PAIRS]; };
+// table [n_pos, 2 n_pairs] fp32: the cosines of row number times frequency, then the sines.
+hipError_t launch_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const RopeFrequencies& f, hipStream_t s);
+// y = x with the pairs (i, i + n_pairs) of each of n_heads heads turned by the table's row pos[axis[i]][row].
+struct RopeAxesArgs {
+  const void* x; void* y;
+  const int32_t* pos; int64_t pos_stride;
+  const float* table; int64_t n_pos;
+  int64_t t, x_stride, y_stride;
+  int32_t n_heads, head_dim, n_pairs;
+  alignas(8) uint8_t axis[ROPE_PAIRS];
+  uint8_t present[ROPE_PAIRS / 8];               // of eight neighbouring pairs: a bit for each axis that one of them follows
+};
+hipError_t launch_rope_axes(const RopeAxesArgs& a, int inverse, hipStream_t s);
+// The residual stream between two blocks (residual.hip): u = post(o) * scale * gate, y = x + u, n = pre(y).  Kinds: 0 LayerNorm, 1 RMSNorm, 2 none.
+struct ResidualArgs {
+  int post_kind, pre_kind, gate_act;             // gate_act: 0 as it is, 1 tanh, 2 sigmoid
+  bool gate_per_row;
+  float post_eps, pre_eps;
+  const void* post_g; const void* post_b; const void* scale; const void* pre_g; const void* pre_b;   // bf16 [d] or null
+  const float* gate;                             // [t] or [1], or null
+  int64_t t; int d;
+};
+hipError_t launch_residual_fwd(const ResidualArgs& a, const void* x, const void* o, void* y, void* n, float* stats, hipStream_t s);
+struct ResidualGrads { float* post_g; float* post_b; float* scale; float* pre_g; float* pre_b; float* gate; };   // null: not wanted
+size_t residual_bwd_partial_floats(int64_t t, int64_t d);
+hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void* dy, const void* y, const void* o, const float* stats, void* dx,
+                               void* d_o, const ResidualGrads& g, int accumulate, float* partial, hipStream_t s);
+// Matrices kept in 8 bits (keep8.hip): q [t, width] bytes, e [t, ceil(width / 32)] exponents; format 0 int8, 1 e4m3.
+hipError_t launch_keep8(const void* x, void* q, void* e, int64_t t, int64_t width, int64_t x_stride, int format, hipStream_t s);
+hipError_t launch_keep8_load(const void* q, const void* e, void* y, int64_t t, int64_t width, int64_t y_stride, int format, hipStream_t s);
+hipError_t launch_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* e, int64_t t, int64_t f, int format, hipStream_t s);
+hipError_t launch_act_bwd_keep8(int act, const void* da, const void* q, const void* e, void* dpre, void* a, int64_t t, int64_t f, int format, hipStream_t s);
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, hipStream_t s);
 
 // Optional per-launch timing with HIP events on the launch stream (off by default).  Classes:

@@ -5,11 +5,13 @@
 #include <hip/hip_runtime.h>
 
 #include <algorithm>
+#include <cmath>
 #include <cstdarg>
 #include <cstdio>
 #include <cstring>
 #include <mutex>
 #include <string>
+#include <utility>
 #include <vector>
 
 #include "../../include/mllm_stage.h"
@@ -575,6 +577,274 @@ mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* t
   const XentArgs a = {logits, targets, dloss, loss, dlogits, t, logits_stride, dlogits_stride, vocab, cols, scale};
   OP_TRY(launch_xent(a, logits_fp32, (hipStream_t)hip_stream));
   return MLLM_OK;
+}
+
+}  // extern "C"
+
+// Positions of packed text and grids.  The walk over the runs, once to check them and once to launch.
+namespace {
+template <typename Run>
+mllm_status_t walk_positions(int32_t n_segments, const int32_t* cu, int32_t n_grids, const int32_t* grids, int64_t* n_pos, Run run) {
+  int64_t most = 0;
+  int32_t g = 0;
+  for (int32_t s = 0; s < n_segments; s++) {
+    if (cu[s + 1] < cu[s]) return op_fail(MLLM_ERR_CU_SEQLENS, "cu_seqlens decreases at segment %d", s);
+    int64_t row = cu[s], p = 0;
+    const int64_t end = cu[s + 1];
+    while (row < end) {
+      PositionRun r = {(int32_t)row, (int32_t)p, 0, 1, 0};
+      const int32_t* grid = grids + 5 * (int64_t)g;
+      int64_t to = end, takes, reaches;
+      if (g < n_grids && grid[0] < row) return op_fail(MLLM_ERR_INDEX, "grid %d begins before the end of the one in front of it", g);
+      if (g < n_grids && grid[0] == row) {
+        const int64_t frames = grid[1], height = grid[2], width = grid[3], step = grid[4];
+        if (frames <= 0 || height <= 0 || width <= 0 || step < 0) return op_fail(MLLM_ERR_SHAPE, "grid %d: sizes must be positive, the step not negative", g);
+        if (height > end - row || width > end - row || frames > end - row || height * width > end - row || frames * height * width > end - row)
+          return op_fail(MLLM_ERR_INDEX, "grid %d goes beyond its segment", g);
+        r.frame_rows = (int32_t)(height * width);
+        r.width = (int32_t)width;
+        r.step = (int32_t)step;
+        to = row + frames * height * width;
+        takes = reaches = std::max((frames - 1) * step + 1, std::max(height, width));
+        g++;
+      } else {
+        if (g < n_grids && grid[0] < end) to = grid[0];
+        takes = reaches = to - row;
+      }
+      if (p + reaches > INT32_MAX) return op_fail(MLLM_ERR_SHAPE, "segment %d: positions beyond 2^31 - 1", s);
+      most = std::max(most, p + reaches);
+      const mllm_status_t st = run(r, to);
+      if (st != MLLM_OK) return st;
+      row = to;
+      p += takes;
+    }
+  }
+  if (g < n_grids) return op_fail(MLLM_ERR_INDEX, "grid %d begins outside the sequence or inside a segment's end", g);
+  if (n_pos) *n_pos = most;
+  return MLLM_OK;
+}
+mllm_status_t check_positions(int32_t n_segments, const int32_t* cu, int32_t n_grids, const int32_t* grids, int64_t* n_pos) {
+  if (!cu || (n_grids > 0 && !grids)) return op_fail(MLLM_ERR_NULL, "cu_seqlens or grids is NULL");
+  if (n_segments < 0 || n_grids < 0) return op_fail(MLLM_ERR_SHAPE, "negative sizes");
+  if (cu[0] != 0) return op_fail(MLLM_ERR_CU_SEQLENS, "cu_seqlens[0] != 0");
+  return walk_positions(n_segments, cu, n_grids, grids, n_pos, [](const PositionRun&, int64_t) { return MLLM_OK; });
+}
+}  // namespace
+
+extern "C" {
+
+mllm_status_t mllm_grid_positions_count(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host, int64_t* n_pos) {
+  if (!n_pos) return op_fail(MLLM_ERR_NULL, "n_pos is NULL");
+  return check_positions(n_segments, cu_seqlens_host, n_grids, grids_host, n_pos);
+}
+
+mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host,
+                                     int32_t* pos, int64_t pos_stride, void* hip_stream) {
+  CHECK(check_positions(n_segments, cu_seqlens_host, n_grids, grids_host, nullptr));
+  const int64_t rows = cu_seqlens_host[n_segments];
+  if (rows > 0 && !pos) return op_fail(MLLM_ERR_NULL, "pos is NULL");
+  if (pos_stride < rows) return op_fail(MLLM_ERR_SHAPE, "pos_stride below the sequence's rows");
+  PositionRuns runs;
+  int count = 0;
+  return walk_positions(n_segments, cu_seqlens_host, n_grids, grids_host, nullptr, [&](const PositionRun& r, int64_t to) {
+    runs.run[count++] = r;
+    if (count == POSITION_RUNS || to == rows) {
+      OP_TRY(launch_grid_positions(runs, count, pos, pos_stride, runs.run[0].row, (int32_t)(to - runs.run[0].row), (hipStream_t)hip_stream));
+      count = 0;
+    }
+    return MLLM_OK;
+  });
+}
+
+mllm_status_t mllm_op_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const double* frequencies_host, void* hip_stream) {
+  if (!frequencies_host || (n_pos > 0 && !table)) return op_fail(MLLM_ERR_NULL, "table or frequencies is NULL");
+  if (n_pairs <= 0 || n_pairs > ROPE_PAIRS) return op_fail(MLLM_ERR_SHAPE, "n_pairs must be in 1 .. %d", ROPE_PAIRS);
+  if (n_pos < 0 || n_pos > MAX_ROWS || n_pos * n_pairs >= (int64_t)1 << 32) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative, n_pos times n_pairs below 2^32");
+  RopeFrequencies f = {};
+  for (int i = 0; i < n_pairs; i++) {
+    f.frequency[i] = frequencies_host[i];
+    if (!std::isfinite(f.frequency[i])) return op_fail(MLLM_ERR_SHAPE, "frequency %d is not finite", i);
+  }
+  OP_TRY(launch_rope_freq_table(table, n_pos, n_pairs, f, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+// Bytes from a matrix's first element to behind its last one (rows of width, stride apart).
+static int64_t span_bytes(int64_t t, int64_t width, int64_t stride, int bytes) {
+  return t <= 0 ? 0 : (int64_t)std::min<__int128>(((__int128)(t - 1) * stride + width) * bytes, INT64_MAX / 4);
+}
+
+mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int64_t pos_stride, int32_t n_axes,
+                                const uint8_t* pair_axis_host, int32_t n_pairs, const float* table, int64_t n_pos, int64_t t,
+                                int32_t n_heads, int32_t head_dim, int64_t x_stride, int64_t y_stride, int inverse, void* hip_stream) {
+  if (!pair_axis_host || !table || (t > 0 && n_heads > 0 && (!x || !y || !pos))) return op_fail(MLLM_ERR_NULL, "a pointer is NULL");
+  if (t < 0 || t > MAX_ROWS || n_heads < 0 || n_heads > 65535 || n_pos < 0 || n_pos > MAX_ROWS)
+    return op_fail(MLLM_ERR_SHAPE, "t, n_heads and n_pos must not be negative, n_heads at most 65535");
+  if (head_dim <= 0 || head_dim % 8 || head_dim > 2 * ROPE_PAIRS) return op_fail(MLLM_ERR_UNSUPPORTED, "head_dim must be a multiple of 8, at most %d", 2 * ROPE_PAIRS);
+  if (n_pairs <= 0 || n_pairs % 8 || 2 * n_pairs > head_dim) return op_fail(MLLM_ERR_SHAPE, "n_pairs must be a positive multiple of 8, at most head_dim / 2");
+  if (n_axes <= 0 || n_axes > ROPE_AXES) return op_fail(MLLM_ERR_UNSUPPORTED, "n_axes must be in 1 .. %d", ROPE_AXES);
+  if (n_axes > 1 && pos_stride < t) return op_fail(MLLM_ERR_SHAPE, "pos_stride below t");
+  const int64_t width = (int64_t)n_heads * head_dim;
+  CHECK(check_rows("x", x, width, x_stride));
+  CHECK(check_rows("y", y, width, y_stride));
+  if ((uintptr_t)table % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "table must start on 16 bytes");
+  if (ranges_overlap(x, span_bytes(t, width, x_stride, 2), y, span_bytes(t, width, y_stride, 2)) && (x != y || x_stride != y_stride))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x (same stride) but not overlap it otherwise");
+  RopeAxesArgs a = {};
+  a.x = x; a.y = y; a.pos = pos; a.pos_stride = pos_stride; a.table = table; a.n_pos = n_pos; a.t = t; a.x_stride = x_stride; a.y_stride = y_stride;
+  a.n_heads = n_heads; a.head_dim = head_dim; a.n_pairs = n_pairs;
+  for (int i = 0; i < n_pairs; i++) {
+    if (pair_axis_host[i] >= n_axes) return op_fail(MLLM_ERR_INDEX, "pair %d follows axis %d of %d", i, (int)pair_axis_host[i], n_axes);
+    a.axis[i] = pair_axis_host[i];
+    a.present[i / 8] |= (uint8_t)(1 << pair_axis_host[i]);
+  }
+  OP_TRY(launch_rope_axes(a, inverse, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+// The residual stream between two blocks.
+namespace {
+mllm_status_t residual_args(const mllm_residual_norm_t* b, int64_t t, int64_t d, ResidualArgs& a) {
+  if (!b) return op_fail(MLLM_ERR_NULL, "block is NULL");
+  if (t < 0 || t > MAX_ROWS || d <= 0 || d % 8 || d > 8192) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, d a multiple of 8, at most 8192");
+  if (b->post_kind < 0 || b->post_kind > MLLM_NORM_NONE || b->pre_kind < 0 || b->pre_kind > MLLM_NORM_NONE) return op_fail(MLLM_ERR_SHAPE, "norm kind out of range");
+  if (b->gate_act < 0 || b->gate_act > MLLM_GATE_SIGMOID) return op_fail(MLLM_ERR_SHAPE, "gate_act out of range");
+  const auto used = [](int32_t kind, const void* p, int32_t from) { return kind <= from ? p : nullptr; };
+  a.post_kind = b->post_kind; a.pre_kind = b->pre_kind; a.gate_act = b->gate_act; a.gate_per_row = b->gate_per_row != 0 && b->gate;
+  a.post_eps = b->post_eps; a.pre_eps = b->pre_eps;
+  a.post_g = used(b->post_kind, b->post_g, MLLM_NORM_RMS); a.post_b = used(b->post_kind, b->post_b, MLLM_NORM_LAYER);
+  a.pre_g = used(b->pre_kind, b->pre_g, MLLM_NORM_RMS); a.pre_b = used(b->pre_kind, b->pre_b, MLLM_NORM_LAYER);
+  a.scale = b->scale; a.gate = b->gate; a.t = t; a.d = (int)d;
+  const auto lacks = [](int32_t kind, const void* g, const void* s) { return kind != MLLM_NORM_NONE && (!g || (kind == MLLM_NORM_LAYER && !s)); };
+  if (lacks(a.post_kind, a.post_g, a.post_b) || lacks(a.pre_kind, a.pre_g, a.pre_b)) return op_fail(MLLM_ERR_NULL, "a norm's gain or shift is NULL");
+  if ((a.post_kind != MLLM_NORM_NONE && !(a.post_eps >= 0.f)) || (a.pre_kind != MLLM_NORM_NONE && !(a.pre_eps >= 0.f)))
+    return op_fail(MLLM_ERR_SHAPE, "eps must not be negative");
+  if (((uintptr_t)a.post_g | (uintptr_t)a.post_b | (uintptr_t)a.pre_g | (uintptr_t)a.pre_b | (uintptr_t)a.scale) % 16)
+    return op_fail(MLLM_ERR_UNSUPPORTED, "gains, shifts and scale must start on 16 bytes");
+  return MLLM_OK;
+}
+struct Range { const void* p; int64_t bytes; };
+bool any_overlap(Range a, std::initializer_list<Range> others) {
+  for (const Range& b : others)
+    if (ranges_overlap(a.p, a.bytes, b.p, b.bytes)) return true;
+  return false;
+}
+}  // namespace
+
+mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const void* x, const void* o, void* y, void* n, float* stats,
+                                        int64_t t, int64_t d, void* hip_stream) {
+  ResidualArgs a;
+  CHECK(residual_args(block, t, d, a));
+  if (a.pre_kind == MLLM_NORM_NONE) n = nullptr;
+  const bool keeps = a.post_kind != MLLM_NORM_NONE || a.pre_kind != MLLM_NORM_NONE;
+  if (t > 0 && (!x || !o || !y || (keeps && !stats) || (a.pre_kind != MLLM_NORM_NONE && !n))) return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
+  if (((uintptr_t)x | (uintptr_t)o | (uintptr_t)y | (uintptr_t)n) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "x, o, y and n must start on 16 bytes");
+  const int64_t bytes = 2 * t * d;
+  const Range rx = {x, bytes}, ro = {o, bytes}, ry = {y, bytes}, rn = {n, bytes}, rs = {keeps ? stats : nullptr, 16 * t};
+  if ((y != x && any_overlap(ry, {rx})) || any_overlap(ry, {ro, rn, rs}) || any_overlap(rn, {rx, ro, rs}) || any_overlap(rs, {rx, ro}))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x; nothing else may overlap");
+  OP_TRY(launch_residual_fwd(a, x, o, y, n, stats, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+size_t mllm_op_residual_norm_bwd_partial_bytes(int64_t t, int64_t d) {
+  return t < 0 || t > MAX_ROWS || d <= 0 || d % 8 || d > 8192 ? 0 : residual_bwd_partial_floats(t, d) * 4;
+}
+
+mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const void* dn, const void* dy, const void* y, const void* o,
+                                        const float* stats, void* dx, void* d_o, const mllm_residual_norm_grads_t* grads, int accumulate,
+                                        float* partial, int64_t t, int64_t d, void* hip_stream) {
+  ResidualArgs a;
+  CHECK(residual_args(block, t, d, a));
+  if (!grads) return op_fail(MLLM_ERR_NULL, "grads is NULL");
+  const bool pre = a.pre_kind != MLLM_NORM_NONE, post = a.post_kind != MLLM_NORM_NONE;
+  if (!pre) dn = y = nullptr;
+  if (!partial || (t > 0 && (!o || !dx || !d_o || (pre && (!dn || !y)) || (!pre && !dy) || ((pre || post) && !stats))))
+    return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
+  if (((uintptr_t)dn | (uintptr_t)dy | (uintptr_t)y | (uintptr_t)o | (uintptr_t)dx | (uintptr_t)d_o | (uintptr_t)partial) % 16)
+    return op_fail(MLLM_ERR_UNSUPPORTED, "dn, dy, y, o, dx, d_o and partial must start on 16 bytes");
+  const int64_t bytes = 2 * t * d;
+  const Range rn = {dn, bytes}, rd = {dy, bytes}, ry = {y, bytes}, ro = {o, bytes}, rx = {dx, bytes}, rdo = {d_o, bytes};
+  const auto bad = [&](Range out) { return (out.p != dn && any_overlap(out, {rn})) || (out.p != dy && any_overlap(out, {rd})) || any_overlap(out, {ry, ro}); };
+  if (any_overlap(rx, {rdo}) || bad(rx) || bad(rdo)) return op_fail(MLLM_ERR_UNSUPPORTED, "dx and d_o may each be dn or dy; nothing else may overlap");
+  ResidualGrads g = {post ? grads->post_g : nullptr, a.post_kind == MLLM_NORM_LAYER ? grads->post_b : nullptr, a.scale ? grads->scale : nullptr,
+                     pre ? grads->pre_g : nullptr, a.pre_kind == MLLM_NORM_LAYER ? grads->pre_b : nullptr, a.gate ? grads->gate : nullptr};
+  const Range out[6] = {{g.post_g, 4 * d}, {g.post_b, 4 * d}, {g.scale, 4 * d}, {g.pre_g, 4 * d}, {g.pre_b, 4 * d}, {g.gate, a.gate_per_row ? 4 * t : 4}};
+  for (int i = 0; i < 6; i++)
+    for (int j = 0; j < i; j++)
+      if (any_overlap(out[i], {out[j]})) return op_fail(MLLM_ERR_UNSUPPORTED, "two gradients overlap");
+  OP_TRY(launch_residual_bwd(a, dn, dy, y, o, stats, dx, d_o, g, accumulate, partial, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+// Matrices kept in 8 bits.
+static mllm_status_t check_keep8(int64_t t, int64_t width, int format) {
+  if (t < 0 || t > MAX_ROWS || width <= 0 || width % 8 || width > ((int64_t)1 << 30)) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, the width a positive multiple of 8, at most 2^30");
+  if (format != MLLM_KEEP_INT8 && format != MLLM_KEEP_E4M3) return op_fail(MLLM_ERR_SHAPE, "unknown 8-bit format");
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_keep8(const void* x, void* q, void* exponents, int64_t t, int64_t width, int64_t x_stride, int format, void* hip_stream) {
+  CHECK(check_keep8(t, width, format));
+  if (t > 0 && (!x || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "x, q or exponents is NULL");
+  CHECK(check_rows("x", x, width, x_stride));
+  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  OP_TRY(launch_keep8(x, q, exponents, t, width, x_stride, format, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_keep8_load(const void* q, const void* exponents, void* y, int64_t t, int64_t width, int64_t y_stride, int format, void* hip_stream) {
+  CHECK(check_keep8(t, width, format));
+  if (t > 0 && (!y || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "y, q or exponents is NULL");
+  CHECK(check_rows("y", y, width, y_stride));
+  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  OP_TRY(launch_keep8_load(q, exponents, y, t, width, y_stride, format, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* exponents, int64_t t, int64_t f, int format, void* hip_stream) {
+  CHECK(check_keep8(t, f, format));
+  if (act < 0 || act > 2) return op_fail(MLLM_ERR_SHAPE, "bad activation arguments");
+  if (t > 0 && (!pre || !a || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "pre, a, q or exponents is NULL");
+  if (((uintptr_t)pre | (uintptr_t)a | (uintptr_t)q) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "pre, a and q must start on 16 bytes");
+  OP_TRY(launch_act_fwd_keep8(act, pre, a, q, exponents, t, f, format, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, const void* exponents, void* dpre, void* a, int64_t t, int64_t f, int format,
+                                    void* hip_stream) {
+  CHECK(check_keep8(t, f, format));
+  if (act < 0 || act > 2) return op_fail(MLLM_ERR_SHAPE, "bad activation arguments");
+  if (t > 0 && (!q || !exponents || !da != !dpre || (!da && !a))) return op_fail(MLLM_ERR_NULL, "q, exponents, da, dpre or a is NULL");
+  if (((uintptr_t)da | (uintptr_t)dpre | (uintptr_t)a | (uintptr_t)q) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "da, dpre, a and q must start on 16 bytes");
+  const int64_t halves = act == 2 ? 2 : 1;
+  if (any_overlap({dpre, 2 * halves * t * f}, {{a, 2 * t * f}}) || any_overlap({a, 2 * t * f}, {{da, 2 * t * f}}) ||
+      (any_overlap({dpre, 2 * halves * t * f}, {{da, 2 * t * f}}) && (dpre != da || halves == 2)))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "dpre may be da for the GELU kinds; nothing else may overlap");
+  OP_TRY(launch_act_bwd_keep8(act, da, q, exponents, dpre, a, t, f, format, (hipStream_t)hip_stream));
+  return MLLM_OK;
+}
+
+size_t mllm_op_linear_bwd_keep8_workspace_bytes(int64_t t, int64_t k, int64_t n) {
+  return t < 0 || t > MAX_ROWS || k <= 0 || n <= 0 || k > ((int64_t)1 << 30) || n > ((int64_t)1 << 30) ? 0 : align_up((size_t)t * k * 2) + linear_bwd_ws_bytes(t, k, n, false);
+}
+
+mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void* exponents, const void* w, void* dx, void* dw, int64_t t,
+                                       int64_t k, int64_t n, int format, int accumulate, void* workspace, size_t workspace_bytes,
+                                       void* hip_stream) {
+  CHECK(check_keep8(t, k, format));
+  if (!dw || !w || (t > 0 && (!dy || !q || !exponents || !dx))) return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
+  if (n <= 0 || n % 8 || n > ((int64_t)1 << 30)) return op_fail(MLLM_ERR_SHAPE, "n must be a positive multiple of 8, at most 2^30");
+  for (const auto& e : {std::pair<int64_t, int64_t>(t, k), std::pair<int64_t, int64_t>(t, n), std::pair<int64_t, int64_t>(k, n)})
+    if (2 * e.first * e.second > GEMM_MAX_OPERAND_BYTES) return op_fail(MLLM_ERR_SHAPE, "an operand of 4 GiB or more");
+  const size_t kept = align_up((size_t)t * k * 2);
+  if (kept && !workspace) return op_fail(MLLM_ERR_NULL, "workspace is NULL");
+  if ((uintptr_t)workspace % ALIGN) return op_fail(MLLM_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
+  if (workspace_bytes < kept) return op_fail(MLLM_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, kept);
+  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  OP_TRY(launch_keep8_load(q, exponents, workspace, t, k, k, format, (hipStream_t)hip_stream));
+  if (t == 0) return mllm_op_linear_bwd(w, w, w, dw, dw, 0, k, n, accumulate, nullptr, nullptr, 0, hip_stream);   // no rows: none of the rows' matrices is touched
+  return mllm_op_linear_bwd(dy, workspace, w, dx, dw, t, k, n, accumulate, nullptr, (char*)workspace + kept, workspace_bytes - kept, hip_stream);
 }
 
 }  // extern "C"

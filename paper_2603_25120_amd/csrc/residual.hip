@@ -1,0 +1,425 @@
+// The residual stream between two blocks of a layer, in one pass over it:
+//   u = post(o) * scale * gate      o the block's output; post LayerNorm, RMSNorm or none; scale of every channel; gate of the block or of every row
+//   y = x + u                       the stream, stored as bf16
+//   n = pre(y)                      what the next block reads: the norm of the stream as it is stored
+// and its gradients.  Bound by memory: o, x, y and n forward, dn, dy, y, o, dx and the gradient of o backward, each once.
+#include <algorithm>
+
+#include "common.h"
+#include "kernels.h"
+#include "rows.h"
+
+namespace mllm {
+
+namespace {
+
+constexpr int LAYER = 0, RMS = 1, NONE = 2;
+
+__device__ __forceinline__ float gate_value(int act, float v) { return act == 1 ? tanhf(v) : act == 2 ? 1.f / (1.f + expf(-v)) : v; }
+__device__ __forceinline__ float gate_slope(int act, float g) { return act == 1 ? 1.f - g * g : act == 2 ? g * (1.f - g) : 1.f; }
+
+// A row belongs to `waves` wavefronts (a lane has eight neighbouring columns, so 512 columns a wavefront), a workgroup to `rows` rows:
+// wavefront w of the workgroup is wavefront w % waves of row w / waves.  Sums over a row go through LDS where it has several wavefronts;
+// every sum has a slot of its own until the next row but one.
+constexpr int MAX_WAVES = 16;
+struct RowSums { float part[2][2][3][MAX_WAVES]; };   // [parity][first or second exchange][sum][wavefront]
+template <int N>
+__device__ __forceinline__ void row_sums(float* v, float (*part)[MAX_WAVES], int waves, int wave, int lane) {
+#pragma unroll
+  for (int i = 0; i < N; i++) v[i] = over_lanes<64, false>(v[i]);
+  if (waves == 1) return;
+  if (lane == 0)
+#pragma unroll
+    for (int i = 0; i < N; i++) part[i][wave] = v[i];
+  __syncthreads();
+  const int first = wave - wave % waves, k = lane & 15;
+#pragma unroll
+  for (int i = 0; i < N; i++) v[i] = over_lanes<16, false>(k < waves ? part[i][first + k] : 0.f);
+}
+
+// (factor, mean) of a norm over the row's values.
+template <int KIND>
+__device__ __forceinline__ void statistics(const float* v, bool there, int d, float eps, float (*part)[3][MAX_WAVES], int waves, int wave, int lane,
+                                           float& factor, float& mean) {
+  factor = 1.f;
+  mean = 0.f;
+  if (KIND == NONE) return;
+  float sum[1];
+  if (KIND == LAYER) {
+    sum[0] = 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) sum[0] += v[e];       // zeros behind the row
+    row_sums<1>(sum, part[0], waves, wave, lane);
+    mean = sum[0] / (float)d;
+  }
+  sum[0] = 0.f;
+  if (there)
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      const float w = v[e] - mean;
+      sum[0] += w * w;
+    }
+  row_sums<1>(sum, part[1], waves, wave, lane);
+  factor = rsqrtf(sum[0] / (float)d + eps);
+}
+
+__device__ __forceinline__ void load_vector(const bf16_t* p, int c, bool there, float* f) {
+  if (p && there) {
+    load8(p + 8 * c, f);
+  } else {
+#pragma unroll
+    for (int e = 0; e < 8; e++) f[e] = 0.f;
+  }
+}
+
+template <int POST, int PRE>
+__global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, const bf16_t* x, const bf16_t* __restrict__ o, bf16_t* y,
+                                                            bf16_t* __restrict__ n, float* __restrict__ stats, int waves, int rows) {
+  __shared__ RowSums sums;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (wave % waves) * 64 + lane;
+  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows + wave / waves;
+  const bool there = row < a.t && c < a.d >> 3;
+  const int64_t at = row * a.d + 8 * c;
+  uint4 uo = make_uint4(0, 0, 0, 0), ux = uo;
+  if (there) {
+    uo = load16_once(o + at);
+    ux = load16_once(x + at);
+  }
+  float v[8], w[8], g[8], b[8];
+  const float gate = a.gate && row < a.t ? gate_value(a.gate_act, a.gate[a.gate_per_row ? row : 0]) : 1.f;
+  unpack8(uo, v);
+  float factor, mean;
+  statistics<POST>(v, there, a.d, a.post_eps, sums.part[0], waves, wave, lane, factor, mean);
+  if (POST != NONE) {
+    load_vector((const bf16_t*)a.post_g, c, there, g);
+    load_vector((const bf16_t*)a.post_b, c, there, b);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] = (v[e] - mean) * factor * g[e] + b[e];
+    if (there && c == 0) {
+      stats[row] = factor;
+      stats[a.t + row] = mean;
+    }
+  }
+  if (a.scale) {
+    load_vector((const bf16_t*)a.scale, c, there, g);
+#pragma unroll
+    for (int e = 0; e < 8; e++) v[e] *= g[e];
+  }
+  unpack8(ux, w);
+#pragma unroll
+  for (int e = 0; e < 8; e++) w[e] = fmaf(v[e], gate, w[e]);
+  const uint4 stored = pack8(w);
+  if (there) store16<false>(y + at, stored);
+  if (PRE == NONE) return;
+  unpack8(stored, w);
+  statistics<PRE>(w, there, a.d, a.pre_eps, sums.part[1], waves, wave, lane, factor, mean);
+  load_vector((const bf16_t*)a.pre_g, c, there, g);
+  load_vector((const bf16_t*)a.pre_b, c, there, b);
+#pragma unroll
+  for (int e = 0; e < 8; e++) w[e] = (w[e] - mean) * factor * g[e] + b[e];
+  if (there) {
+    store16<false>(n + at, pack8(w));
+    if (c == 0) {
+      stats[2 * a.t + row] = factor;
+      stats[3 * a.t + row] = mean;
+    }
+  }
+}
+
+// Backward.  With h the stream without mean, times its factor, z the same of o (o itself without a norm), g the gate:
+//   dY = dy + pre'(dn),  pre'(dn) = factor * (dn pre_g - mean(dn pre_g) - h mean(dn pre_g h));  dx = dY
+//   do = post'(dY g scale post_g), or dY g scale without a norm
+// and, summed over the rows, A = dY g z and B = dY g of every column: post_g's gradient is scale A, post_b's scale B, the scale's
+// post_g A + post_b B; pre_g's and pre_b's are the sums of dn h and dn.  The gate's is the row's sum of dY post(o) scale times its slope.
+// A workgroup goes over rows b, b + B, ...; a lane keeps its columns' four sums, which go to `partial`, [set][workgroup][d]; the next row's
+// operands are requested before a row is worked on.
+template <int POST, int PRE>
+__global__ __launch_bounds__(1024) void residual_bwd_kernel(ResidualArgs a, const bf16_t* dn, const bf16_t* dy, const bf16_t* __restrict__ y,
+                                                            const bf16_t* __restrict__ o, const float* __restrict__ stats, bf16_t* dx, bf16_t* d_o,
+                                                            float* __restrict__ gate_rows, float* __restrict__ partial, int waves, int rows, int sets) {
+  __shared__ RowSums sums;
+  __shared__ float joined_columns[8 * 512];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (wave % waves) * 64 + lane, of = wave / waves;
+  const bool column = c < a.d >> 3;
+  const int64_t step = (int64_t)gridDim.x * rows;
+  float k[8], kb[8], A[8], Bs[8], C[8], D[8];   // B and D only where a norm has a shift
+  uint4 pg = make_uint4(0, 0, 0, 0);
+  if (PRE != NONE && column) pg = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_g + 8 * c);
+  {   // k: what dY g is multiplied by on its way through gain and scale; kb: what the norm's shift contributes to the gate's gradient
+    float g[8], s[8];
+    load_vector((const bf16_t*)a.post_g, c, column, g);
+    load_vector((const bf16_t*)a.scale, c, column, s);
+    load_vector((const bf16_t*)a.post_b, c, column, kb);
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      k[e] = (a.post_g ? g[e] : 1.f) * (a.scale ? s[e] : 1.f);
+      kb[e] *= a.scale ? s[e] : 1.f;
+      A[e] = Bs[e] = C[e] = D[e] = 0.f;
+    }
+  }
+  float gate_sum = 0.f;
+  uint4 qn, qd, qy, qo;
+  float f_pre, m_pre, f_post, m_post, gate_in;
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    qn = qd = qy = qo = make_uint4(0, 0, 0, 0);
+    f_pre = f_post = m_pre = m_post = gate_in = 0.f;
+    if (row >= a.t) return;
+    const int64_t at = row * a.d + 8 * c;
+    if (column) {
+      if (PRE != NONE) qn = load16_once(dn + at);
+      if (PRE != NONE) qy = load16_once(y + at);
+      if (dy) qd = load16_once(dy + at);
+      qo = load16_once(o + at);
+    }
+    if (PRE != NONE) f_pre = stats[2 * a.t + row];
+    if (PRE == LAYER) m_pre = stats[3 * a.t + row];
+    if (POST != NONE) f_post = stats[row];
+    if (POST == LAYER) m_post = stats[a.t + row];
+    if (a.gate) gate_in = a.gate[a.gate_per_row ? row : 0];
+  };
+  const int64_t first = (int64_t)blockIdx.x * rows;
+  fetch(first + of);
+  int parity = 0;
+  for (int64_t base = first; base < a.t; base += step, parity ^= 1) {    // all wavefronts alike: they meet at barriers
+    const int64_t row = base + of, at = row * a.d + 8 * c;
+    const bool there = row < a.t && column;
+    const float r1 = f_pre, m1 = m_pre, r2 = f_post, m2 = m_post;
+    const float gate = a.gate ? gate_value(a.gate_act, gate_in) : 1.f;
+    float dY[8], h[8], z[8];
+    unpack8(qd, dY);
+    unpack8(qo, z);
+    float s[3];
+    if (PRE != NONE) {
+      float dh[8], gain[8];
+      unpack8(pg, gain);
+      unpack8(qn, dh);
+      unpack8(qy, h);
+      s[0] = s[1] = 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; e++) {
+        h[e] = (h[e] - m1) * r1;
+        C[e] = fmaf(dh[e], h[e], C[e]);
+        if (PRE == LAYER) D[e] += dh[e];
+        dh[e] *= gain[e];
+        s[0] = fmaf(dh[e], h[e], s[0]);
+        if (PRE == LAYER) s[1] += dh[e];
+      }
+      fetch(row + step);
+      row_sums<PRE == LAYER ? 2 : 1>(s, sums.part[parity][0], waves, wave, lane);
+      s[0] /= (float)a.d;
+      s[1] = PRE == LAYER ? s[1] / (float)a.d : 0.f;
+#pragma unroll
+      for (int e = 0; e < 8; e++) dY[e] = fmaf(dh[e] - s[1] - h[e] * s[0], r1, dY[e]);
+    } else {
+      fetch(row + step);
+    }
+    if (there) store16<false>(dx + at, pack8(dY));
+    s[0] = s[1] = s[2] = 0.f;
+    float dz[8];
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      if (POST != NONE) z[e] = (z[e] - m2) * r2;
+      const float v = dY[e] * gate;
+      A[e] = fmaf(v, z[e], A[e]);
+      if (POST == LAYER) Bs[e] += v;
+      dz[e] = dY[e] * k[e];
+      s[0] = fmaf(dz[e], z[e], s[0]);
+      if (POST == LAYER) s[1] += dz[e];
+      if (POST == LAYER) s[2] = fmaf(dY[e], kb[e], s[2]);
+    }
+    if (POST != NONE || a.gate) {
+      row_sums<POST == LAYER ? 3 : 1>(s, sums.part[parity][1], waves, wave, lane);
+      if (gate_rows && row < a.t) {
+        const float v = (s[0] + (POST == LAYER ? s[2] : 0.f)) * gate_slope(a.gate_act, gate);
+        if (a.gate_per_row) {
+          if (c == 0) gate_rows[row] = v;
+        } else {
+          gate_sum += v;
+        }
+      }
+    }
+    const float t0 = POST != NONE ? s[0] / (float)a.d : 0.f, t1 = POST == LAYER ? s[1] / (float)a.d : 0.f;
+#pragma unroll
+    for (int e = 0; e < 8; e++) {
+      if (POST != NONE) dz[e] = (dz[e] - t1 - z[e] * t0) * r2;
+      dz[e] *= gate;
+    }
+    if (there) store16<false>(d_o + at, pack8(dz));
+  }
+  // Sets of sums in the order of the bits of `sets`; the wavefronts of a column add theirs up through LDS.
+  const int64_t W = gridDim.x;
+  int at_set = 0;
+#pragma unroll
+  for (int set = 0; set < 4; set++) {
+    if (!(sets >> set & 1) || (set == 1 && POST != LAYER) || (set == 3 && PRE != LAYER)) continue;   // those are not among the sets
+    float* v = set == 0 ? A : set == 1 ? Bs : set == 2 ? C : D;
+    if (rows > 1) {
+      __syncthreads();
+#pragma unroll
+      for (int e = 0; e < 8; e++) joined_columns[wave * 512 + e * 64 + lane] = v[e];
+      __syncthreads();
+      if (of == 0)
+        for (int r = 1; r < rows; r++)
+#pragma unroll
+          for (int e = 0; e < 8; e++) v[e] += joined_columns[(r * waves + wave) * 512 + e * 64 + lane];
+    }
+    if (of == 0 && column) {
+      float4* p = reinterpret_cast<float4*>(partial + ((int64_t)at_set * W + blockIdx.x) * a.d + 8 * c);
+      p[0] = make_float4(v[0], v[1], v[2], v[3]);
+      p[1] = make_float4(v[4], v[5], v[6], v[7]);
+    }
+    at_set++;
+  }
+  if (gate_rows && !a.gate_per_row) {
+    __syncthreads();
+    if (wave % waves == 0 && lane == 0) joined_columns[of] = gate_sum;
+    __syncthreads();
+    if (threadIdx.x == 0) {
+      float v = 0.f;
+      for (int r = 0; r < rows; r++) v += joined_columns[r];
+      gate_rows[blockIdx.x] = v;
+    }
+  }
+}
+
+// What the sums of the workgroups come to: 32 columns a workgroup as in reduce_partials_kernel (32 slices of the rows, added pairwise).
+// Grid y: A and B with the gradients that follow from both, C, D, the shared gate.
+struct FinishArgs {
+  const float* partial; const float* gate_partial;
+  int W, d, sets, accumulate;
+  const bf16_t* post_g; const bf16_t* post_b; const bf16_t* scale;
+  ResidualGrads g;
+};
+__device__ __forceinline__ float4 finish_sum(const float* partial, int W, int d, int64_t col, bool valid, float4 (*part)[8], int slice, int cg) {
+  float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
+  if (valid)
+    for (int p = slice; p < W; p += 8 * 32) {
+      float4 v[8];
+#pragma unroll
+      for (int q = 0; q < 8; q++) v[q] = p + 32 * q < W ? *reinterpret_cast<const float4*>(partial + (int64_t)(p + 32 * q) * d + col) : make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int q = 0; q < 8; q++) { s.x += v[q].x; s.y += v[q].y; s.z += v[q].z; s.w += v[q].w; }
+    }
+  __syncthreads();
+  part[slice][cg] = s;
+  __syncthreads();
+#pragma unroll
+  for (int half = 16; half >= 1; half >>= 1) {
+    if (slice < half) {
+      const float4 a = part[slice][cg], b = part[slice + half][cg];
+      part[slice][cg] = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
+    }
+    __syncthreads();
+  }
+  return part[0][cg];
+}
+__global__ __launch_bounds__(256) void residual_finish_kernel(FinishArgs a) {
+  __shared__ float4 part[32][8];
+  const int cg = threadIdx.x & 7, slice = threadIdx.x >> 3, job = blockIdx.y;
+  const int64_t col = ((int64_t)blockIdx.x * 8 + cg) * 4;
+  const bool valid = col < a.d;
+  auto put = [&](float* out, const float* v) {
+    if (!out || slice != 0 || !valid) return;
+#pragma unroll
+    for (int e = 0; e < 4; e++) out[col + e] = v[e] + (a.accumulate ? out[col + e] : 0.f);
+  };
+  if (job == 3) {        // the shared gate: one workgroup
+    if (!a.gate_partial || blockIdx.x != 0) return;
+    float v = 0.f;
+    for (int p = threadIdx.x; p < a.W; p += 256) v += a.gate_partial[p];
+    float* red = reinterpret_cast<float*>(part);
+    red[threadIdx.x] = v;
+    __syncthreads();
+    for (int half = 128; half >= 1; half >>= 1) {
+      if (threadIdx.x < half) red[threadIdx.x] += red[threadIdx.x + half];
+      __syncthreads();
+    }
+    if (threadIdx.x == 0) *a.g.gate = red[0] + (a.accumulate ? *a.g.gate : 0.f);
+    return;
+  }
+  const int before = __popc(a.sets & ((1 << (job == 0 ? 0 : job + 1)) - 1));
+  const float* sums = a.partial + (int64_t)before * a.W * a.d;
+  if (job > 0) {
+    if (!(a.sets >> (job + 1) & 1)) return;
+    const float4 s = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
+    const float v[4] = {s.x, s.y, s.z, s.w};
+    put(job == 1 ? a.g.pre_g : a.g.pre_b, v);
+    return;
+  }
+  if (!(a.sets & 3)) return;
+  float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
+  if (a.sets & 1) {
+    A = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
+    sums += (int64_t)a.W * a.d;
+  }
+  if (a.sets & 2) B = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
+  if (!valid) return;
+  const float va[4] = {A.x, A.y, A.z, A.w}, vb[4] = {B.x, B.y, B.z, B.w};
+  float pg[4], pb[4], sc[4];
+#pragma unroll
+  for (int e = 0; e < 4; e++) {
+    const float s = a.scale ? bf16lo(a.scale[col + e]) : 1.f, g = a.post_g ? bf16lo(a.post_g[col + e]) : 1.f, b = a.post_b ? bf16lo(a.post_b[col + e]) : 0.f;
+    pg[e] = s * va[e];
+    pb[e] = s * vb[e];
+    sc[e] = a.post_b ? fmaf(g, va[e], b * vb[e]) : g * va[e];
+  }
+  put(a.g.post_g, pg);
+  put(a.g.post_b, pb);
+  put(a.g.scale, sc);
+}
+
+// Wavefronts of a row, rows of a workgroup: eight wavefronts or more.
+inline int row_waves(int64_t d) { return (int)ceil_div(d, 512); }
+inline int rows_of(int waves) { return std::max(1, 8 / waves); }
+// Workgroups of the backward pass: 16 wavefronts a CU, each going over several rows.
+inline int64_t bwd_workgroups(int64_t t, int64_t d) {
+  const int waves = row_waves(d), rows = rows_of(waves);
+  const int64_t most = (int64_t)256 * std::max(1, 16 / (waves * rows));
+  return std::max<int64_t>(1, std::min(most, ceil_div(t, rows)));
+}
+
+}  // namespace
+
+hipError_t launch_residual_fwd(const ResidualArgs& a, const void* x, const void* o, void* y, void* n, float* stats, hipStream_t s) {
+  if (a.t == 0) return hipSuccess;
+  const int waves = row_waves(a.d), rows = rows_of(waves);
+  const int64_t blocks = ceil_div(a.t, rows);
+  const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID)), block(64 * waves * rows);
+  ProfScope prof(PROF_ELEMENTWISE, (a.pre_kind == NONE ? 6.0 : 8.0) * (double)a.t * a.d, s);
+#define CALL(POST, PRE)                                                                                                                \
+  if (a.post_kind == POST && a.pre_kind == PRE)                                                                                        \
+    hipLaunchKernelGGL((residual_fwd_kernel<POST, PRE>), grid, block, 0, s, a, (const bf16_t*)x, (const bf16_t*)o, (bf16_t*)y, (bf16_t*)n, stats, waves, rows);
+  CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
+#undef CALL
+  return hipGetLastError();
+}
+
+size_t residual_bwd_partial_floats(int64_t t, int64_t d) { return (size_t)bwd_workgroups(t, d) * (size_t)(4 * d + 1); }
+
+hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void* dy, const void* y, const void* o, const float* stats, void* dx,
+                               void* d_o, const ResidualGrads& g, int accumulate, float* partial, hipStream_t s) {
+  const int waves = row_waves(a.d), rows = rows_of(waves);
+  const int64_t W = bwd_workgroups(a.t, a.d);
+  // which of A, B, C, D anybody asks for
+  const int sets = (g.post_g || g.scale ? 1 : 0) | (g.post_b || (g.scale && a.post_b) ? 2 : 0) | (g.pre_g ? 4 : 0) | (g.pre_b ? 8 : 0);
+  float* gate_partial = g.gate && !a.gate_per_row ? partial + (size_t)__builtin_popcount(sets) * W * a.d : nullptr;
+  float* gate_rows = a.gate_per_row ? g.gate : gate_partial;
+  {
+    ProfScope prof(PROF_ELEMENTWISE, (4.0 + (dy ? 2 : 0) + (a.pre_kind == NONE ? 0 : 4) + 2) * (double)a.t * a.d, s);
+#define CALL(POST, PRE)                                                                                                              \
+    if (a.post_kind == POST && a.pre_kind == PRE)                                                                                    \
+      hipLaunchKernelGGL((residual_bwd_kernel<POST, PRE>), dim3((unsigned)W), dim3(64 * waves * rows), 0, s, a, (const bf16_t*)dn, (const bf16_t*)dy, \
+                         (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, sets);
+    CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
+#undef CALL
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+  }
+  if (!sets && !gate_partial) return hipSuccess;
+  FinishArgs f = {partial, gate_partial, (int)W, a.d, sets, accumulate, (const bf16_t*)a.post_g, (const bf16_t*)a.post_b, (const bf16_t*)a.scale, g};
+  ProfScope prof(PROF_ELEMENTWISE, 0.0, s);   // the bytes of the sums are counted with their first stage
+  hipLaunchKernelGGL(residual_finish_kernel, dim3((unsigned)ceil_div(a.d, 32), 4), dim3(256), 0, s, f);
+  return hipGetLastError();
+}
+
+}  // namespace mllm
