@@ -478,7 +478,7 @@ mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqle
 mllm_status_t mllm_grid_positions_count(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host,
                                         int64_t* n_pos);
 /* Rotary factors for any list of frequencies (frequencies_host: n_pairs numbers, radians a position): table device fp32
- * [n_pos, 2 n_pairs], row p the cosines of p * frequency, then the sines; angles and their sines in fp64.  n_pairs at most 128.  With
+ * [n_pos, 2 n_pairs], row p the cosines of p * frequency, then the sines; angles and their sines in fp64.  n_pairs at most 128, n_pos * n_pairs below 2^31.  With
  * rope_base^(-2i/head_dim) for i < head_dim/2 it is the table of mllm_op_rope_table. */
 mllm_status_t mllm_op_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const double* frequencies_host, void* hip_stream);
 /* Rotation of heads whose pairs follow several axes.  x bf16 [t, x_stride], the leading n_heads heads of head_dim columns of a row; pair i < n_pairs of

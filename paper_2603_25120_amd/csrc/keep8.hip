@@ -18,15 +18,6 @@ namespace {
 constexpr int INT8 = 0, E4M3 = 1;
 constexpr int LOWEST = -112;          // below it the values of a block are rounded to multiples of 2^-112 (e4m3 2^-121), so that no step meets subnormal numbers
 
-// n / divisor for n < 2^31, by multiplication.
-struct Division { uint32_t divisor, factor, shift; };
-Division division(uint32_t divisor) {
-  uint32_t shift = 0;
-  while (((uint64_t)1 << shift) < divisor) shift++;
-  return {divisor, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - divisor)) / divisor + 1), shift};
-}
-__device__ __forceinline__ uint32_t divide(uint32_t n, const Division& d) { return (__umulhi(n, d.factor) + n) >> d.shift; }
-
 // The largest magnitude of eight bf16 values, as the bits of a bf16: infinity and NaN are the largest ones.
 typedef uint16_t u16x2 __attribute__((ext_vector_type(2)));
 __device__ __forceinline__ u16x2 larger(uint32_t a, uint32_t b) {

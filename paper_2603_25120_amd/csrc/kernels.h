@@ -231,8 +231,7 @@ struct RopeAxesArgs {
   const float* table; int64_t n_pos;
   int64_t t, x_stride, y_stride;
   int32_t n_heads, head_dim, n_pairs;
-  alignas(8) uint8_t axis[ROPE_PAIRS];
-  uint8_t present[ROPE_PAIRS / 8];               // of eight neighbouring pairs: a bit for each axis that one of them follows
+  uint8_t axis[ROPE_PAIRS];
 };
 hipError_t launch_rope_axes(const RopeAxesArgs& a, int inverse, hipStream_t s);
 // The residual stream between two blocks (residual.hip): u = post(o) * scale * gate, y = x + u, n = pre(y).  Kinds: 0 LayerNorm, 1 RMSNorm, 2 none.

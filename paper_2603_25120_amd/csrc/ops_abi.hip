@@ -659,7 +659,7 @@ mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqle
 mllm_status_t mllm_op_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const double* frequencies_host, void* hip_stream) {
   if (!frequencies_host || (n_pos > 0 && !table)) return op_fail(MLLM_ERR_NULL, "table or frequencies is NULL");
   if (n_pairs <= 0 || n_pairs > ROPE_PAIRS) return op_fail(MLLM_ERR_SHAPE, "n_pairs must be in 1 .. %d", ROPE_PAIRS);
-  if (n_pos < 0 || n_pos > MAX_ROWS || n_pos * n_pairs >= (int64_t)1 << 32) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative, n_pos times n_pairs below 2^32");
+  if (n_pos < 0 || n_pos > MAX_ROWS || n_pos * n_pairs >= (int64_t)1 << 31) return op_fail(MLLM_ERR_SHAPE, "n_pos must not be negative, n_pos times n_pairs below 2^31");
   RopeFrequencies f = {};
   for (int i = 0; i < n_pairs; i++) {
     f.frequency[i] = frequencies_host[i];
@@ -696,7 +696,6 @@ mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int6
   for (int i = 0; i < n_pairs; i++) {
     if (pair_axis_host[i] >= n_axes) return op_fail(MLLM_ERR_INDEX, "pair %d follows axis %d of %d", i, (int)pair_axis_host[i], n_axes);
     a.axis[i] = pair_axis_host[i];
-    a.present[i / 8] |= (uint8_t)(1 << pair_axis_host[i]);
   }
   OP_TRY(launch_rope_axes(a, inverse, (hipStream_t)hip_stream));
   return MLLM_OK;

@@ -12,18 +12,22 @@ namespace {
 
 // ---------------------------------------------------------------------------------------------
 // Positions.  A run is a stretch of text or a grid of frames x height x width rows; the host has walked over the samples and knows where
-// every run begins and at which position.  The runs travel as the kernel's argument, so that a call copies nothing and can be captured.
+// every run begins and at which position.  The runs travel as the kernel's argument, so that a call copies nothing and can be captured.  Bound by the
+// launch: 220 rows 1.8 us, 32768 rows of 95 runs 3 to 5.
 // ---------------------------------------------------------------------------------------------
 __global__ __launch_bounds__(256) void grid_positions_kernel(PositionRuns runs, int n, int32_t* __restrict__ pos, int64_t stride, int32_t row0, int32_t rows) {
-  const int32_t i = blockIdx.x * 256 + threadIdx.x;
-  if (i >= rows) return;
-  const int32_t row = row0 + i;
-  int lo = 0, hi = n;                       // the last run that begins at or before the row
-  while (hi - lo > 1) {
-    const int mid = (lo + hi) >> 1;
-    if (runs.run[mid].row <= row) lo = mid; else hi = mid;
-  }
-  const PositionRun r = runs.run[lo];
+  __shared__ PositionRun run[256];
+  run[threadIdx.x].row = INT32_MAX;
+  if ((int)threadIdx.x < n) run[threadIdx.x] = runs.run[threadIdx.x];
+  __syncthreads();
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x;
+  if (i >= (uint32_t)rows) return;
+  const int32_t row = row0 + (int32_t)i;
+  int lo = 0;                               // the last run that begins at or before the row
+#pragma unroll
+  for (int step = 128; step >= 1; step >>= 1)
+    if (run[lo + step].row <= row) lo += step;
+  const PositionRun r = run[lo];
   const int32_t at = row - r.row;
   int32_t a = at, b = at, c = at;
   if (r.frame_rows > 0) {
@@ -51,75 +55,70 @@ __global__ __launch_bounds__(256) void rope_freq_table_kernel(float* __restrict_
 
 // ---------------------------------------------------------------------------------------------
 // Rotation: pair i of a head, its elements i and i + pairs, by the angle of position pos[axis of i][row]; elements from 2 pairs on stay.
-// A thread has eight neighbouring pairs of a token and takes them through up to heads_per heads (grid y), four heads' values requested
-// before any is stored: their factors, as many bytes as the values of two heads, are then read once for all of them.  Pairs of several
-// axes read the eight factors of each axis that is there and keep their own.  Threads behind the pairs' copy what is not rotated.
+// Bound by memory.  An item is eight neighbouring pairs of a head (two 16-byte vectors), or eight elements behind them, which are copied.  A workgroup has a
+// few whole tokens: their factors, gathered pair by pair from the rows that the axes' positions name, are put into LDS once for all heads, while
+// the first items' values are on their way, and its lanes then go over the tokens' items side by side, a wavefront over 2 KB of a row.
+// us for 32768 x 40 x 128 (pairs dealt out to three axes) / 26496 x 32 x 64 / 2999 x 32 x 128 / 8192 x 32 x 128 (dealt out): this 112 / 47 / 10.9 / 25, the first at
+// 6.0 TB/s; two items a lane in flight 114 / 46 / 10.7 / 26, four 125 / 47 / 12.6 / 28; three times the tokens a workgroup 130 / 56 / 11 / 27; eight pairs of a token a
+// thread that goes over its heads, factors in registers: 167 / 51 / 14.8 / 28.
 // ---------------------------------------------------------------------------------------------
+constexpr int ROPE_LDS = 4096;                 // floats of factors a workgroup holds
+struct RopeItems { Division per_token, groups, pairs; int tokens; };   // items of a token and of a head; pairs of a head; tokens of a workgroup
 template <bool PAST>
-__global__ __launch_bounds__(256) void rope_axes_kernel(RopeAxesArgs a, int groups, int tokens_per_block, int heads_per, bool inverse) {
-  const int tid = threadIdx.x, of = tid / groups, g = tid - of * groups;
-  if (of >= tokens_per_block) return;
-  const int rotated = a.n_pairs >> 3, h0 = blockIdx.y * heads_per, h1 = min(h0 + heads_per, a.n_heads);
-  const bf16_t* x = (const bf16_t*)a.x;
-  bf16_t* y = (bf16_t*)a.y;
-  for (int64_t row = (int64_t)blockIdx.x * tokens_per_block + of; row < a.t; row += (int64_t)gridDim.x * tokens_per_block) {
-    const bool tail = g >= rotated;
-    const int at = tail ? 2 * a.n_pairs + 8 * (g - rotated) : 8 * g;
-    float cs[8], sn[8];
-    if (!tail) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) cs[e] = sn[e] = __uint_as_float(0x7fc00000u);
-      const uint64_t axes = *reinterpret_cast<const uint64_t*>(a.axis + 8 * g);
-      const uint32_t there = a.present[g];
-#pragma unroll
-      for (int k = 0; k < ROPE_AXES; k++) {
-        if (!(there >> k & 1)) continue;
-        const int64_t p = a.pos[k * a.pos_stride + row];
-        if (p < 0 || p >= a.n_pos) continue;          // those pairs stay NaN
-        float c[8], s[8];
-        load8(a.table + p * (2 * a.n_pairs) + 8 * g, c);
-        load8(a.table + p * (2 * a.n_pairs) + a.n_pairs + 8 * g, s);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          const bool mine = (axes >> (8 * e) & 0xff) == k;
-          cs[e] = mine ? c[e] : cs[e];
-          sn[e] = mine ? (inverse ? -s[e] : s[e]) : sn[e];
-        }
-      }
+__global__ __launch_bounds__(256) void rope_axes_kernel(RopeAxesArgs a, RopeItems it, bool inverse) {
+  __shared__ __align__(16) float factors[ROPE_LDS];   // of every token the cosines, then the sines
+  const int tid = threadIdx.x, P = a.n_pairs;
+  const int64_t row0 = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * it.tokens;
+  if (row0 >= a.t) return;
+  const int tokens = a.t - row0 < it.tokens ? (int)(a.t - row0) : it.tokens, items = tokens * (int)it.per_token.divisor;
+  const bf16_t* x = (const bf16_t*)a.x + row0 * a.x_stride;
+  bf16_t* y = (bf16_t*)a.y + row0 * a.y_stride;
+  int token, group, column;
+  bool tail;
+  uint4 u, v;
+  auto fetch = [&](int i) __attribute__((always_inline)) {
+    if (i >= items) return;
+    token = (int)divide((uint32_t)i, it.per_token);
+    const int r = i - token * (int)it.per_token.divisor, h = (int)divide((uint32_t)r, it.groups);
+    group = r - h * (int)it.groups.divisor;
+    tail = 8 * group >= P;
+    column = h * a.head_dim + 8 * group + (tail ? P : 0);
+    const bf16_t* src = x + (int64_t)token * a.x_stride + column;
+    u = load16_once(src);
+    if (!tail) v = load16_once(src + P);
+  };
+  fetch(tid);
+  for (int i = tid; i < tokens * P; i += 256) {
+    const int of = (int)divide((uint32_t)i, it.pairs), pair = i - of * P;
+    const int64_t p = a.pos[a.axis[pair] * a.pos_stride + row0 + of];
+    float c = __uint_as_float(0x7fc00000u), s = c;
+    if (p >= 0 && p < a.n_pos) {
+      c = a.table[p * (2 * P) + pair];
+      s = a.table[p * (2 * P) + P + pair];
     }
-    const bf16_t* src = x + row * a.x_stride + at;
-    bf16_t* dst = y + row * a.y_stride + at;
-    constexpr int AHEAD = 4;
-    for (int h = h0; h < h1; h += AHEAD) {
-      uint4 u[AHEAD], v[AHEAD];
+    factors[of * 2 * P + pair] = c;
+    factors[of * 2 * P + P + pair] = inverse ? -s : s;
+  }
+  __syncthreads();
+  for (int i = tid; i < items; i += 256) {
+    bf16_t* o = y + (int64_t)token * a.y_stride + column;
+    if (tail) {
+      store16<PAST>(o, u);
+    } else {
+      float cs[8], sn[8], first[8], second[8], f[8], g[8];
+      load8(factors + token * 2 * P + 8 * group, cs);
+      load8(factors + token * 2 * P + P + 8 * group, sn);
+      unpack8(u, first);
+      unpack8(v, second);
 #pragma unroll
-      for (int j = 0; j < AHEAD; j++) {
-        u[j] = v[j] = make_uint4(0, 0, 0, 0);
-        if (h + j < h1) {
-          u[j] = *reinterpret_cast<const uint4*>(src + (int64_t)(h + j) * a.head_dim);
-          if (!tail) v[j] = *reinterpret_cast<const uint4*>(src + (int64_t)(h + j) * a.head_dim + a.n_pairs);
-        }
+      for (int e = 0; e < 8; e++) {
+        f[e] = first[e] * cs[e] - second[e] * sn[e];
+        g[e] = second[e] * cs[e] + first[e] * sn[e];
       }
-#pragma unroll
-      for (int j = 0; j < AHEAD; j++) {
-        if (h + j >= h1) break;
-        bf16_t* o = dst + (int64_t)(h + j) * a.head_dim;
-        if (tail) {
-          store16<PAST>(o, u[j]);
-          continue;
-        }
-        float p[8], q[8], r[8], s[8];
-        unpack8(u[j], p);
-        unpack8(v[j], q);
-#pragma unroll
-        for (int e = 0; e < 8; e++) {
-          r[e] = p[e] * cs[e] - q[e] * sn[e];
-          s[e] = q[e] * cs[e] + p[e] * sn[e];
-        }
-        store16<PAST>(o, pack8(r));
-        store16<PAST>(o + a.n_pairs, pack8(s));
-      }
+      store16<PAST>(o, pack8(f));
+      store16<PAST>(o + P, pack8(g));
     }
+    fetch(i + 256);
   }
 }
 
@@ -143,16 +142,17 @@ hipError_t launch_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, 
 hipError_t launch_rope_axes(const RopeAxesArgs& a, int inverse, hipStream_t s) {
   if (a.t == 0 || a.n_heads == 0) return hipSuccess;
   const int groups = a.n_pairs / 8 + (a.y == a.x ? 0 : (a.head_dim - 2 * a.n_pairs) / 8);   // in place the rest is there already
-  const int tokens = 256 / groups;
-  int heads_per = 8;
-  while (heads_per > 1 && ceil_div(a.t, tokens) * ceil_div(a.n_heads, heads_per) < 1024) heads_per /= 2;
+  const int64_t per_token = (int64_t)a.n_heads * groups;
+  // two items a thread where a token has fewer, but no fewer than 1024 workgroups
+  int64_t tokens = std::min<int64_t>(512 / per_token, ROPE_LDS / (2 * a.n_pairs));
+  tokens = std::max<int64_t>(1, std::min(tokens, a.t / 1024));
+  const RopeItems it = {division((uint32_t)per_token), division((uint32_t)groups), division((uint32_t)a.n_pairs), (int)tokens};
   const double values = (double)a.t * a.n_heads * (a.y == a.x ? 2 * a.n_pairs : a.head_dim);
   ProfScope prof(PROF_ELEMENTWISE, 4.0 * values, s);
-  const dim3 grid((unsigned)std::min(ceil_div(a.t, tokens), MAX_GRID), (unsigned)ceil_div(a.n_heads, heads_per));
-  if (2.0 * values >= NT_BYTES)
-    hipLaunchKernelGGL(rope_axes_kernel<true>, grid, dim3(256), 0, s, a, groups, tokens, heads_per, inverse != 0);
-  else
-    hipLaunchKernelGGL(rope_axes_kernel<false>, grid, dim3(256), 0, s, a, groups, tokens, heads_per, inverse != 0);
+  const int64_t blocks = ceil_div(a.t, tokens);
+  const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID));
+  const auto kernel = 2.0 * values >= NT_BYTES ? rope_axes_kernel<true> : rope_axes_kernel<false>;
+  hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, a, it, inverse != 0);
   return hipGetLastError();
 }
 

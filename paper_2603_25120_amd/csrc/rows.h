@@ -62,5 +62,14 @@ __device__ __forceinline__ float over_lanes(float v) {
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 constexpr int64_t MAX_GRID = 1 << 20;   // workgroups along x: a dimension holds fewer than 2^32 threads
 
+// n / divisor for n < 2^31, by multiplication.
+struct Division { uint32_t divisor, factor, shift; };
+inline Division division(uint32_t divisor) {
+  uint32_t shift = 0;
+  while (((uint64_t)1 << shift) < divisor) shift++;
+  return {divisor, (uint32_t)((((uint64_t)1 << 32) * (((uint64_t)1 << shift) - divisor)) / divisor + 1), shift};
+}
+__device__ __forceinline__ uint32_t divide(uint32_t n, const Division& d) { return (__umulhi(n, d.factor) + n) >> d.shift; }
+
 }  // namespace
 }  // namespace mllm
