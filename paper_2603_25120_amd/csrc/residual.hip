@@ -37,7 +37,8 @@ __device__ __forceinline__ void row_sums(float* v, float (*part)[MAX_WAVES], int
   for (int i = 0; i < N; i++) v[i] = over_lanes<16, false>(k < waves ? part[i][first + k] : 0.f);
 }
 
-// (factor, mean) of a norm over the row's values.
+// (factor, mean) of a norm over the row's values.  LayerNorm takes two exchanges, the mean and then the squares about it (every wavefront's mean and squares joined in
+// one exchange: 5125 x 3200 with LayerNorm on both sides 34.9 us, so 33.1).
 template <int KIND>
 __device__ __forceinline__ void statistics(const float* v, bool there, int d, float eps, float (*part)[3][MAX_WAVES], int waves, int wave, int lane,
                                            float& factor, float& mean) {
@@ -72,56 +73,77 @@ __device__ __forceinline__ void load_vector(const bf16_t* p, int c, bool there, 
   }
 }
 
-template <int POST, int PRE>
+template <int POST, int PRE, bool PAST>
 __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, const bf16_t* x, const bf16_t* __restrict__ o, bf16_t* y,
                                                             bf16_t* __restrict__ n, float* __restrict__ stats, int waves, int rows) {
-  __shared__ RowSums sums;
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (wave % waves) * 64 + lane;
-  const int64_t row = ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * rows + wave / waves;
-  const bool there = row < a.t && c < a.d >> 3;
-  const int64_t at = row * a.d + 8 * c;
-  uint4 uo = make_uint4(0, 0, 0, 0), ux = uo;
-  if (there) {
-    uo = load16_once(o + at);
-    ux = load16_once(x + at);
-  }
-  float v[8], w[8], g[8], b[8];
-  const float gate = a.gate && row < a.t ? gate_value(a.gate_act, a.gate[a.gate_per_row ? row : 0]) : 1.f;
-  unpack8(uo, v);
-  float factor, mean;
-  statistics<POST>(v, there, a.d, a.post_eps, sums.part[0], waves, wave, lane, factor, mean);
-  if (POST != NONE) {
-    load_vector((const bf16_t*)a.post_g, c, there, g);
-    load_vector((const bf16_t*)a.post_b, c, there, b);
-#pragma unroll
-    for (int e = 0; e < 8; e++) v[e] = (v[e] - mean) * factor * g[e] + b[e];
-    if (there && c == 0) {
-      stats[row] = factor;
-      stats[a.t + row] = mean;
+  __shared__ RowSums sums[2];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (wave % waves) * 64 + lane, of = wave / waves;
+  const bool column = c < a.d >> 3;
+  const int64_t step = (int64_t)gridDim.x * rows;
+  uint4 qo, qx;
+  float gate_in = 0.f;
+  auto fetch = [&](int64_t row) __attribute__((always_inline)) {
+    qo = qx = make_uint4(0, 0, 0, 0);
+    if (row >= a.t) return;
+    if (column) {
+      qo = load16_once(o + row * a.d + 8 * c);
+      qx = load16_once(x + row * a.d + 8 * c);
     }
+    if (a.gate) gate_in = a.gate[a.gate_per_row ? row : 0];
+  };
+  const int64_t first = (int64_t)blockIdx.x * rows;
+  fetch(first + of);
+  uint4 pg = make_uint4(0, 0, 0, 0), pb = pg, sc = pg, ng = pg, nb = pg;
+  if (column) {
+    if (POST != NONE) pg = *reinterpret_cast<const uint4*>((const bf16_t*)a.post_g + 8 * c);
+    if (POST == LAYER) pb = *reinterpret_cast<const uint4*>((const bf16_t*)a.post_b + 8 * c);
+    if (a.scale) sc = *reinterpret_cast<const uint4*>((const bf16_t*)a.scale + 8 * c);
+    if (PRE != NONE) ng = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_g + 8 * c);
+    if (PRE == LAYER) nb = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_b + 8 * c);
   }
-  if (a.scale) {
-    load_vector((const bf16_t*)a.scale, c, there, g);
+  int parity = 0;
+  for (int64_t base = first; base < a.t; base += step, parity ^= 1) {    // all wavefronts alike: they meet at barriers
+    const int64_t row = base + of, at = row * a.d + 8 * c;
+    const bool there = row < a.t && column;
+    const float gate = a.gate ? gate_value(a.gate_act, gate_in) : 1.f;
+    float v[8], w[8], g[8], b[8];
+    unpack8(qo, v);
+    unpack8(qx, w);
+    fetch(row + step);
+    float factor, mean;
+    statistics<POST>(v, there, a.d, a.post_eps, sums[parity].part[0], waves, wave, lane, factor, mean);
+    if (POST != NONE) {
+      unpack8(pg, g);
+      unpack8(pb, b);
 #pragma unroll
-    for (int e = 0; e < 8; e++) v[e] *= g[e];
-  }
-  unpack8(ux, w);
+      for (int e = 0; e < 8; e++) v[e] = (v[e] - mean) * factor * g[e] + (POST == LAYER ? b[e] : 0.f);
+      if (there && c == 0) {
+        stats[row] = factor;
+        stats[a.t + row] = mean;
+      }
+    }
+    if (a.scale) {
+      unpack8(sc, g);
 #pragma unroll
-  for (int e = 0; e < 8; e++) w[e] = fmaf(v[e], gate, w[e]);
-  const uint4 stored = pack8(w);
-  if (there) store16<false>(y + at, stored);
-  if (PRE == NONE) return;
-  unpack8(stored, w);
-  statistics<PRE>(w, there, a.d, a.pre_eps, sums.part[1], waves, wave, lane, factor, mean);
-  load_vector((const bf16_t*)a.pre_g, c, there, g);
-  load_vector((const bf16_t*)a.pre_b, c, there, b);
+      for (int e = 0; e < 8; e++) v[e] *= g[e];
+    }
 #pragma unroll
-  for (int e = 0; e < 8; e++) w[e] = (w[e] - mean) * factor * g[e] + b[e];
-  if (there) {
-    store16<false>(n + at, pack8(w));
-    if (c == 0) {
-      stats[2 * a.t + row] = factor;
-      stats[3 * a.t + row] = mean;
+    for (int e = 0; e < 8; e++) w[e] = fmaf(v[e], gate, w[e]);
+    const uint4 stored = pack8(w);
+    if (there) store16<PAST>(y + at, stored);
+    if (PRE == NONE) continue;
+    unpack8(stored, w);
+    statistics<PRE>(w, there, a.d, a.pre_eps, sums[parity].part[1], waves, wave, lane, factor, mean);
+    unpack8(ng, g);
+    unpack8(nb, b);
+#pragma unroll
+    for (int e = 0; e < 8; e++) w[e] = (w[e] - mean) * factor * g[e] + (PRE == LAYER ? b[e] : 0.f);
+    if (there) {
+      store16<PAST>(n + at, pack8(w));
+      if (c == 0) {
+        stats[2 * a.t + row] = factor;
+        stats[3 * a.t + row] = mean;
+      }
     }
   }
 }
@@ -133,27 +155,25 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
 // post_g A + post_b B; pre_g's and pre_b's are the sums of dn h and dn.  The gate's is the row's sum of dY post(o) scale times its slope.
 // A workgroup goes over rows b, b + B, ...; a lane keeps its columns' four sums, which go to `partial`, [set][workgroup][d]; the next row's
 // operands are requested before a row is worked on.
-template <int POST, int PRE>
-__global__ __launch_bounds__(1024) void residual_bwd_kernel(ResidualArgs a, const bf16_t* dn, const bf16_t* dy, const bf16_t* __restrict__ y,
+template <int POST, int PRE, bool PAST, int THREADS>
+__global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, const bf16_t* dn, const bf16_t* dy, const bf16_t* __restrict__ y,
                                                             const bf16_t* __restrict__ o, const float* __restrict__ stats, bf16_t* dx, bf16_t* d_o,
                                                             float* __restrict__ gate_rows, float* __restrict__ partial, int waves, int rows, int sets) {
   __shared__ RowSums sums;
   __shared__ float joined_columns[8 * 512];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, c = (wave % waves) * 64 + lane, of = wave / waves;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (wave % waves) * 64 + lane, of = wave / waves;
   const bool column = c < a.d >> 3;
   const int64_t step = (int64_t)gridDim.x * rows;
-  float k[8], kb[8], A[8], Bs[8], C[8], D[8];   // B and D only where a norm has a shift
+  float k[8], A[8], Bs[8], C[8], D[8];   // B and D only where a norm has a shift
   uint4 pg = make_uint4(0, 0, 0, 0);
   if (PRE != NONE && column) pg = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_g + 8 * c);
-  {   // k: what dY g is multiplied by on its way through gain and scale; kb: what the norm's shift contributes to the gate's gradient
+  {   // k: what dY g is multiplied by on its way through gain and scale
     float g[8], s[8];
     load_vector((const bf16_t*)a.post_g, c, column, g);
     load_vector((const bf16_t*)a.scale, c, column, s);
-    load_vector((const bf16_t*)a.post_b, c, column, kb);
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       k[e] = (a.post_g ? g[e] : 1.f) * (a.scale ? s[e] : 1.f);
-      kb[e] *= a.scale ? s[e] : 1.f;
       A[e] = Bs[e] = C[e] = D[e] = 0.f;
     }
   }
@@ -213,7 +233,7 @@ __global__ __launch_bounds__(1024) void residual_bwd_kernel(ResidualArgs a, cons
     } else {
       fetch(row + step);
     }
-    if (there) store16<false>(dx + at, pack8(dY));
+    if (there) store16<PAST>(dx + at, pack8(dY));
     s[0] = s[1] = s[2] = 0.f;
     float dz[8];
 #pragma unroll
@@ -225,7 +245,13 @@ __global__ __launch_bounds__(1024) void residual_bwd_kernel(ResidualArgs a, cons
       dz[e] = dY[e] * k[e];
       s[0] = fmaf(dz[e], z[e], s[0]);
       if (POST == LAYER) s[1] += dz[e];
-      if (POST == LAYER) s[2] = fmaf(dY[e], kb[e], s[2]);
+    }
+    if (POST == LAYER && gate_rows) {   // the norm's shift counts for the gate alone: read again for every row rather than kept
+      float b[8], sc[8];
+      load_vector((const bf16_t*)a.post_b, c, column, b);
+      load_vector((const bf16_t*)a.scale, c, column, sc);
+#pragma unroll
+      for (int e = 0; e < 8; e++) s[2] = fmaf(dY[e], a.scale ? b[e] * sc[e] : b[e], s[2]);
     }
     if (POST != NONE || a.gate) {
       row_sums<POST == LAYER ? 3 : 1>(s, sums.part[parity][1], waves, wave, lane);
@@ -244,7 +270,7 @@ __global__ __launch_bounds__(1024) void residual_bwd_kernel(ResidualArgs a, cons
       if (POST != NONE) dz[e] = (dz[e] - t1 - z[e] * t0) * r2;
       dz[e] *= gate;
     }
-    if (there) store16<false>(d_o + at, pack8(dz));
+    if (there) store16<PAST>(d_o + at, pack8(dz));
   }
   // Sets of sums in the order of the bits of `sets`; the wavefronts of a column add theirs up through LDS.
   const int64_t W = gridDim.x;
@@ -371,11 +397,20 @@ __global__ __launch_bounds__(256) void residual_finish_kernel(FinishArgs a) {
 // Wavefronts of a row, rows of a workgroup: eight wavefronts or more.
 inline int row_waves(int64_t d) { return (int)ceil_div(d, 512); }
 inline int rows_of(int waves) { return std::max(1, 8 / waves); }
-// Workgroups of the backward pass: 16 wavefronts a CU, each going over several rows.
+// Workgroups, each going over several rows.  Backward one a CU, two where a wavefront has a row of its own (us with 256 and 512: 32768 x 4096 268 and 290,
+// 5125 x 3200 42.6 and 43.4, 2999 x 3584 30.7 and 31.6, 777 x 4096 15.9 and 18, 26496 x 1024 64 and 67.6; 30000 x 256 26.7 and 24); with the next row but one requested too,
+// the same.
 inline int64_t bwd_workgroups(int64_t t, int64_t d) {
-  const int waves = row_waves(d), rows = rows_of(waves);
-  const int64_t most = (int64_t)256 * std::max(1, 16 / (waves * rows));
-  return std::max<int64_t>(1, std::min(most, ceil_div(t, rows)));
+  const int waves = row_waves(d);
+  return std::max<int64_t>(1, std::min<int64_t>(waves == 1 ? 512 : 256, ceil_div(t, rows_of(waves))));
+}
+// Forward as many of 768 as gives all of them the same number of rows (5125 x 3200 25.1 us, with 256 29.2, a row each 29.1; 2999 x 3584 16.5, 20.3, 20.1; 30000 x 256 14.9,
+// 19.8, 17.1); where the results go past the caches as backward (32768 x 4096 183, with 768 198, a row each 181; 16000 x 8192 176, 178, 233; 65000 x 2048 178, 198,
+// 179; 500000 x 256 with 512 197, 256 262, 768 199).
+inline int64_t fwd_workgroups(int64_t t, int64_t d, bool past) {
+  const int waves = row_waves(d);
+  const int64_t blocks = ceil_div(t, rows_of(waves)), most = !past ? 768 : waves == 1 ? 512 : 256;
+  return ceil_div(blocks, ceil_div(blocks, most));
 }
 
 }  // namespace
@@ -383,12 +418,12 @@ inline int64_t bwd_workgroups(int64_t t, int64_t d) {
 hipError_t launch_residual_fwd(const ResidualArgs& a, const void* x, const void* o, void* y, void* n, float* stats, hipStream_t s) {
   if (a.t == 0) return hipSuccess;
   const int waves = row_waves(a.d), rows = rows_of(waves);
-  const int64_t blocks = ceil_div(a.t, rows);
-  const dim3 grid((unsigned)std::min(blocks, MAX_GRID), (unsigned)ceil_div(blocks, MAX_GRID)), block(64 * waves * rows);
+  const bool past = 2 * a.t * a.d >= NT_BYTES;
+  const dim3 grid((unsigned)fwd_workgroups(a.t, a.d, past)), block(64 * waves * rows);
   ProfScope prof(PROF_ELEMENTWISE, (a.pre_kind == NONE ? 6.0 : 8.0) * (double)a.t * a.d, s);
 #define CALL(POST, PRE)                                                                                                                \
   if (a.post_kind == POST && a.pre_kind == PRE)                                                                                        \
-    hipLaunchKernelGGL((residual_fwd_kernel<POST, PRE>), grid, block, 0, s, a, (const bf16_t*)x, (const bf16_t*)o, (bf16_t*)y, (bf16_t*)n, stats, waves, rows);
+    hipLaunchKernelGGL((past ? residual_fwd_kernel<POST, PRE, true> : residual_fwd_kernel<POST, PRE, false>), grid, block, 0, s, a, (const bf16_t*)x, (const bf16_t*)o, (bf16_t*)y, (bf16_t*)n, stats, waves, rows);
   CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
 #undef CALL
   return hipGetLastError();
@@ -406,9 +441,10 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void
   float* gate_rows = a.gate_per_row ? g.gate : gate_partial;
   {
     ProfScope prof(PROF_ELEMENTWISE, (4.0 + (dy ? 2 : 0) + (a.pre_kind == NONE ? 0 : 4) + 2) * (double)a.t * a.d, s);
+    const bool past = 2 * a.t * a.d >= NT_BYTES;
 #define CALL(POST, PRE)                                                                                                              \
     if (a.post_kind == POST && a.pre_kind == PRE)                                                                                    \
-      hipLaunchKernelGGL((residual_bwd_kernel<POST, PRE>), dim3((unsigned)W), dim3(64 * waves * rows), 0, s, a, (const bf16_t*)dn, (const bf16_t*)dy, \
+      hipLaunchKernelGGL((64 * waves * rows <= 512 ? (past ? residual_bwd_kernel<POST, PRE, true, 512> : residual_bwd_kernel<POST, PRE, false, 512>) : (past ? residual_bwd_kernel<POST, PRE, true, 1024> : residual_bwd_kernel<POST, PRE, false, 1024>)), dim3((unsigned)W), dim3(64 * waves * rows), 0, s, a, (const bf16_t*)dn, (const bf16_t*)dy, \
                          (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, sets);
     CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
 #undef CALL
