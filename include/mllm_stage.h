@@ -537,14 +537,16 @@ mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const
  * e, the smallest from -112 on with max |x| <= L * 2^e, and q holds x * 2^-e rounded to the nearest (ties to even) of the format:
  * MLLM_KEEP_INT8 whole numbers, L = 127; MLLM_KEEP_E4M3 8-bit floating point (OCP E4M3), L = 448.  The exponent's byte is e + 127.  The values
  * q * 2^e are bf16 numbers, so nothing else is rounded (2^128, to which numbers from 3.28e38 on may be rounded, comes back as an infinity).
- * A block that holds an infinity or a NaN has the byte 255 and comes back as NaN. */
+ * A block that holds an infinity or a NaN has the byte 255 and comes back as NaN.
+ * q and exponents may not overlap each other or another tensor of a call. */
 enum { MLLM_KEEP_INT8 = 0, MLLM_KEEP_E4M3 = 1 };
 mllm_status_t mllm_op_keep8(const void* x, void* q, void* exponents, int64_t t, int64_t width, int64_t x_stride, int format,
                             void* hip_stream);
 mllm_status_t mllm_op_keep8_load(const void* q, const void* exponents, void* y, int64_t t, int64_t width, int64_t y_stride, int format,
                                  void* hip_stream);
 /* mllm_op_act_fwd that keeps what the activation is taken of in 8 bits: pre [t, f], or for SwiGLU [gate | up] [t, 2f], each half in blocks of its own:
- * q [t, f] or [t, 2f], exponents [t, ceil(f / 32)] or [t, 2 ceil(f / 32)].  a bf16 [t, f] comes from pre itself. */
+ * q [t, f] or [t, 2f], exponents [t, ceil(f / 32)] or [t, 2 ceil(f / 32)].  a bf16 [t, f] comes from pre itself and may not
+ * overlap it. */
 mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* exponents, int64_t t, int64_t f, int format,
                                     void* hip_stream);
 /* mllm_op_act_bwd from there: dpre (like pre) from da [t, f] and the kept values; a [t, f] (or NULL) receives the activation of the kept values, which the
@@ -553,7 +555,8 @@ mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, 
 mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, const void* exponents, void* dpre, void* a, int64_t t,
                                     int64_t f, int format, void* hip_stream);
 /* mllm_op_linear_bwd with x [t, k] kept in 8 bits by mllm_op_keep8.  workspace: mllm_op_linear_bwd_keep8_workspace_bytes, 256-byte aligned; with
- * less a product may be cut into fewer parts, below 2 t k bytes (rounded up to 256) the call is refused. */
+ * less a product may be cut into fewer parts, below 2 t k bytes (rounded up to 256) the call is refused.  dx, dw and workspace may not overlap
+ * each other or an input. */
 size_t mllm_op_linear_bwd_keep8_workspace_bytes(int64_t t, int64_t k, int64_t n);
 mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void* exponents, const void* w, void* dx, void* dw, int64_t t,
                                        int64_t k, int64_t n, int format, int accumulate, void* workspace, size_t workspace_bytes,

@@ -776,7 +776,14 @@ mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const
   return MLLM_OK;
 }
 
-// Matrices kept in 8 bits.
+// Matrices kept in 8 bits.  Nothing that a call reads or writes beside them may share a byte with them.
+static mllm_status_t check_kept(const void* q, const void* exponents, int64_t t, int64_t width, std::initializer_list<Range> others, int64_t parts = 1) {
+  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  const Range values = {q, t * width * parts}, bytes = {exponents, t * ((width + 31) / 32) * parts};
+  if (any_overlap(values, {bytes}) || any_overlap(values, others) || any_overlap(bytes, others))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "q and exponents may not overlap each other or another tensor");
+  return MLLM_OK;
+}
 static mllm_status_t check_keep8(int64_t t, int64_t width, int format) {
   if (t < 0 || t > MAX_ROWS || width <= 0 || width % 8 || width > ((int64_t)1 << 30)) return op_fail(MLLM_ERR_SHAPE, "t must not be negative, the width a positive multiple of 8, at most 2^30");
   if (format != MLLM_KEEP_INT8 && format != MLLM_KEEP_E4M3) return op_fail(MLLM_ERR_SHAPE, "unknown 8-bit format");
@@ -787,7 +794,7 @@ mllm_status_t mllm_op_keep8(const void* x, void* q, void* exponents, int64_t t, 
   CHECK(check_keep8(t, width, format));
   if (t > 0 && (!x || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "x, q or exponents is NULL");
   CHECK(check_rows("x", x, width, x_stride));
-  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  CHECK(check_kept(q, exponents, t, width, {{x, span_bytes(t, width, x_stride, 2)}}));
   OP_TRY(launch_keep8(x, q, exponents, t, width, x_stride, format, (hipStream_t)hip_stream));
   return MLLM_OK;
 }
@@ -796,7 +803,7 @@ mllm_status_t mllm_op_keep8_load(const void* q, const void* exponents, void* y, 
   CHECK(check_keep8(t, width, format));
   if (t > 0 && (!y || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "y, q or exponents is NULL");
   CHECK(check_rows("y", y, width, y_stride));
-  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  CHECK(check_kept(q, exponents, t, width, {{y, span_bytes(t, width, y_stride, 2)}}));
   OP_TRY(launch_keep8_load(q, exponents, y, t, width, y_stride, format, (hipStream_t)hip_stream));
   return MLLM_OK;
 }
@@ -805,7 +812,10 @@ mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, 
   CHECK(check_keep8(t, f, format));
   if (act < 0 || act > 2) return op_fail(MLLM_ERR_SHAPE, "bad activation arguments");
   if (t > 0 && (!pre || !a || !q || !exponents)) return op_fail(MLLM_ERR_NULL, "pre, a, q or exponents is NULL");
-  if (((uintptr_t)pre | (uintptr_t)a | (uintptr_t)q) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "pre, a and q must start on 16 bytes");
+  if (((uintptr_t)pre | (uintptr_t)a) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "pre and a must start on 16 bytes");
+  const int64_t halves = act == 2 ? 2 : 1;
+  CHECK(check_kept(q, exponents, t, f, {{pre, 2 * halves * t * f}, {a, 2 * t * f}}, halves));
+  if (any_overlap({pre, 2 * halves * t * f}, {{a, 2 * t * f}})) return op_fail(MLLM_ERR_UNSUPPORTED, "a may not overlap pre");
   OP_TRY(launch_act_fwd_keep8(act, pre, a, q, exponents, t, f, format, (hipStream_t)hip_stream));
   return MLLM_OK;
 }
@@ -815,8 +825,9 @@ mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, cons
   CHECK(check_keep8(t, f, format));
   if (act < 0 || act > 2) return op_fail(MLLM_ERR_SHAPE, "bad activation arguments");
   if (t > 0 && (!q || !exponents || !da != !dpre || (!da && !a))) return op_fail(MLLM_ERR_NULL, "q, exponents, da, dpre or a is NULL");
-  if (((uintptr_t)da | (uintptr_t)dpre | (uintptr_t)a | (uintptr_t)q) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "da, dpre, a and q must start on 16 bytes");
+  if (((uintptr_t)da | (uintptr_t)dpre | (uintptr_t)a) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "da, dpre and a must start on 16 bytes");
   const int64_t halves = act == 2 ? 2 : 1;
+  CHECK(check_kept(q, exponents, t, f, {{da, 2 * t * f}, {dpre, 2 * halves * t * f}, {a, 2 * t * f}}, halves));
   if (any_overlap({dpre, 2 * halves * t * f}, {{a, 2 * t * f}}) || any_overlap({a, 2 * t * f}, {{da, 2 * t * f}}) ||
       (any_overlap({dpre, 2 * halves * t * f}, {{da, 2 * t * f}}) && (dpre != da || halves == 2)))
     return op_fail(MLLM_ERR_UNSUPPORTED, "dpre may be da for the GELU kinds; nothing else may overlap");
@@ -840,7 +851,10 @@ mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void
   if (kept && !workspace) return op_fail(MLLM_ERR_NULL, "workspace is NULL");
   if ((uintptr_t)workspace % ALIGN) return op_fail(MLLM_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   if (workspace_bytes < kept) return op_fail(MLLM_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, kept);
-  if ((uintptr_t)q % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "q must start on 16 bytes");
+  CHECK(check_kept(q, exponents, t, k, {{dx, 2 * t * k}, {dw, 4 * k * n}, {workspace, (int64_t)workspace_bytes}}));
+  const Range rx = {dx, 2 * t * k}, rw = {dw, 4 * k * n}, rs = {workspace, (int64_t)workspace_bytes}, in[2] = {{dy, 2 * t * n}, {w, 2 * k * n}};
+  if (any_overlap(rx, {rw, rs, in[0], in[1]}) || any_overlap(rw, {rs, in[0], in[1]}) || any_overlap(rs, {in[0], in[1]}))
+    return op_fail(MLLM_ERR_UNSUPPORTED, "dx, dw and workspace may not overlap each other or an input");
   OP_TRY(launch_keep8_load(q, exponents, workspace, t, k, k, format, (hipStream_t)hip_stream));
   if (t == 0) return mllm_op_linear_bwd(w, w, w, dw, dw, 0, k, n, accumulate, nullptr, nullptr, 0, hip_stream);   // no rows: none of the rows' matrices is touched
   return mllm_op_linear_bwd(dy, workspace, w, dx, dw, t, k, n, accumulate, nullptr, (char*)workspace + kept, workspace_bytes - kept, hip_stream);

@@ -16,7 +16,11 @@ namespace {
 constexpr int LAYER = 0, RMS = 1, NONE = 2;
 
 __device__ __forceinline__ float gate_value(int act, float v) { return act == 1 ? tanhf(v) : act == 2 ? 1.f / (1.f + expf(-v)) : v; }
-__device__ __forceinline__ float gate_slope(int act, float g) { return act == 1 ? 1.f - g * g : act == 2 ? g * (1.f - g) : 1.f; }
+__device__ __forceinline__ float gate_slope(int act, float v) {   // from the gate itself: 1 - tanh^2 and s (1 - s) have no digits left where they are small
+  if (act == 0) return 1.f;
+  const float e = expf(act == 1 ? -2.f * fabsf(v) : -fabsf(v)), r = 1.f / (1.f + e);
+  return (act == 1 ? 4.f : 1.f) * e * r * r;
+}
 
 // A row belongs to `waves` wavefronts (a lane has eight neighbouring columns, so 512 columns a wavefront), a workgroup to `rows` rows:
 // wavefront w of the workgroup is wavefront w % waves of row w / waves.  Sums over a row go through LDS where it has several wavefronts;
@@ -204,7 +208,7 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
     const int64_t row = base + of, at = row * a.d + 8 * c;
     const bool there = row < a.t && column;
     const float r1 = f_pre, m1 = m_pre, r2 = f_post, m2 = m_post;
-    const float gate = a.gate ? gate_value(a.gate_act, gate_in) : 1.f;
+    const float gate_raw = gate_in, gate = a.gate ? gate_value(a.gate_act, gate_in) : 1.f;
     float dY[8], h[8], z[8];
     unpack8(qd, dY);
     unpack8(qo, z);
@@ -256,7 +260,7 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
     if (POST != NONE || a.gate) {
       row_sums<POST == LAYER ? 3 : 1>(s, sums.part[parity][1], waves, wave, lane);
       if (gate_rows && row < a.t) {
-        const float v = (s[0] + (POST == LAYER ? s[2] : 0.f)) * gate_slope(a.gate_act, gate);
+        const float v = (s[0] + (POST == LAYER ? s[2] : 0.f)) * gate_slope(a.gate_act, gate_raw);
         if (a.gate_per_row) {
           if (c == 0) gate_rows[row] = v;
         } else {
@@ -308,7 +312,8 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
   }
 }
 
-// What the sums of the workgroups come to: 32 columns a workgroup as in reduce_partials_kernel (32 slices of the rows, added pairwise).
+// What the sums of the workgroups come to: 32 columns a workgroup, a line of 128 bytes, four of them a lane, and every 32nd workgroup's sums in a group of eight
+// lanes, eight of those requested at a time; the groups of a wavefront are added up by exchanges, the wavefronts' sums through LDS.
 // Grid y: A and B with the gradients that follow from both, C, D, the shared gate.
 struct FinishArgs {
   const float* partial; const float* gate_partial;
@@ -316,7 +321,15 @@ struct FinishArgs {
   const bf16_t* post_g; const bf16_t* post_b; const bf16_t* scale;
   ResidualGrads g;
 };
-__device__ __forceinline__ float4 finish_sum(const float* partial, int W, int d, int64_t col, bool valid, float4 (*part)[8], int slice, int cg) {
+__device__ __forceinline__ float over_groups(float v) {   // lanes 8, 16, ... apart
+  v += from_lane<0x128>(v);
+  auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  v = __uint_as_float(w[0]) + __uint_as_float(w[1]);
+  w = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return __uint_as_float(w[0]) + __uint_as_float(w[1]);
+}
+__device__ __forceinline__ void finish_sum(const float* partial, int W, int d, int64_t col, bool valid, float (*part)[8][4], float* out) {
+  const int cg = threadIdx.x & 7, slice = threadIdx.x >> 3, wave = threadIdx.x >> 6;
   float4 s = make_float4(0.f, 0.f, 0.f, 0.f);
   if (valid)
     for (int p = slice; p < W; p += 8 * 32) {
@@ -326,68 +339,55 @@ __device__ __forceinline__ float4 finish_sum(const float* partial, int W, int d,
 #pragma unroll
       for (int q = 0; q < 8; q++) { s.x += v[q].x; s.y += v[q].y; s.z += v[q].z; s.w += v[q].w; }
     }
-  __syncthreads();
-  part[slice][cg] = s;
+  s = make_float4(over_groups(s.x), over_groups(s.y), over_groups(s.z), over_groups(s.w));
+  if ((threadIdx.x & 63) < 8) *reinterpret_cast<float4*>(part[wave][cg]) = s;
   __syncthreads();
 #pragma unroll
-  for (int half = 16; half >= 1; half >>= 1) {
-    if (slice < half) {
-      const float4 a = part[slice][cg], b = part[slice + half][cg];
-      part[slice][cg] = make_float4(a.x + b.x, a.y + b.y, a.z + b.z, a.w + b.w);
-    }
-    __syncthreads();
-  }
-  return part[0][cg];
+  for (int e = 0; e < 4; e++) out[e] = (part[0][cg][e] + part[1][cg][e]) + (part[2][cg][e] + part[3][cg][e]);
 }
 __global__ __launch_bounds__(256) void residual_finish_kernel(FinishArgs a) {
-  __shared__ float4 part[32][8];
-  const int cg = threadIdx.x & 7, slice = threadIdx.x >> 3, job = blockIdx.y;
+  __shared__ __align__(16) float part[2][4][8][4];
+  const int cg = threadIdx.x & 7, job = blockIdx.y;
   const int64_t col = ((int64_t)blockIdx.x * 8 + cg) * 4;
   const bool valid = col < a.d;
   auto put = [&](float* out, const float* v) {
-    if (!out || slice != 0 || !valid) return;
+    if (!out || threadIdx.x >= 8 || !valid) return;
 #pragma unroll
     for (int e = 0; e < 4; e++) out[col + e] = v[e] + (a.accumulate ? out[col + e] : 0.f);
   };
   if (job == 3) {        // the shared gate: one workgroup
     if (!a.gate_partial || blockIdx.x != 0) return;
-    float v = 0.f;
+    float v = 0.f, *red = &part[0][0][0][0];
     for (int p = threadIdx.x; p < a.W; p += 256) v += a.gate_partial[p];
-    float* red = reinterpret_cast<float*>(part);
-    red[threadIdx.x] = v;
+    v = over_lanes<64, false>(v);
+    if ((threadIdx.x & 63) == 0) red[threadIdx.x >> 6] = v;
     __syncthreads();
-    for (int half = 128; half >= 1; half >>= 1) {
-      if (threadIdx.x < half) red[threadIdx.x] += red[threadIdx.x + half];
-      __syncthreads();
-    }
-    if (threadIdx.x == 0) *a.g.gate = red[0] + (a.accumulate ? *a.g.gate : 0.f);
+    if (threadIdx.x == 0) *a.g.gate = (red[0] + red[1]) + (red[2] + red[3]) + (a.accumulate ? *a.g.gate : 0.f);
     return;
   }
   const int before = __popc(a.sets & ((1 << (job == 0 ? 0 : job + 1)) - 1));
   const float* sums = a.partial + (int64_t)before * a.W * a.d;
   if (job > 0) {
     if (!(a.sets >> (job + 1) & 1)) return;
-    const float4 s = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
-    const float v[4] = {s.x, s.y, s.z, s.w};
+    float v[4];
+    finish_sum(sums, a.W, a.d, col, valid, part[0], v);
     put(job == 1 ? a.g.pre_g : a.g.pre_b, v);
     return;
   }
   if (!(a.sets & 3)) return;
-  float4 A = make_float4(0.f, 0.f, 0.f, 0.f), B = A;
+  float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, pg[4], pb[4], sc[4];
   if (a.sets & 1) {
-    A = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
+    finish_sum(sums, a.W, a.d, col, valid, part[0], A);
     sums += (int64_t)a.W * a.d;
   }
-  if (a.sets & 2) B = finish_sum(sums, a.W, a.d, col, valid, part, slice, cg);
+  if (a.sets & 2) finish_sum(sums, a.W, a.d, col, valid, part[1], B);
   if (!valid) return;
-  const float va[4] = {A.x, A.y, A.z, A.w}, vb[4] = {B.x, B.y, B.z, B.w};
-  float pg[4], pb[4], sc[4];
 #pragma unroll
   for (int e = 0; e < 4; e++) {
     const float s = a.scale ? bf16lo(a.scale[col + e]) : 1.f, g = a.post_g ? bf16lo(a.post_g[col + e]) : 1.f, b = a.post_b ? bf16lo(a.post_b[col + e]) : 0.f;
-    pg[e] = s * va[e];
-    pb[e] = s * vb[e];
-    sc[e] = a.post_b ? fmaf(g, va[e], b * vb[e]) : g * va[e];
+    pg[e] = s * A[e];
+    pb[e] = s * B[e];
+    sc[e] = a.post_b ? fmaf(g, A[e], b * B[e]) : g * A[e];
   }
   put(a.g.post_g, pg);
   put(a.g.post_b, pb);

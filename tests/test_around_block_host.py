@@ -147,6 +147,7 @@ KEEP = dict(q=2 * P, exponents=3 * P, t=4, format=0)
     (NULL, dict(x=None)), (NULL, dict(q=None)), (NULL, dict(exponents=None)), (SHAPE, dict(t=-1)), (SHAPE, dict(width=0)), (SHAPE, dict(width=60)),
     (SHAPE, dict(width=(1 << 30) + 8)), (SHAPE, dict(format=2)), (SHAPE, dict(format=-1)), (SHAPE, dict(x_stride=56)), (SHAPE, dict(x_stride=68)),
     (UNSUPPORTED, dict(x=P + 8)), (UNSUPPORTED, dict(q=2 * P + 8)),
+    (UNSUPPORTED, dict(q=P + 496)), (UNSUPPORTED, dict(exponents=P + 511)), (UNSUPPORTED, dict(exponents=2 * P + 255)),
 ])
 def test_keep8_refusals(B, status, change):
     refused(B, status, B.mllm_op_keep8, **{**KEEP, **dict(x=P, width=64), **change})
@@ -157,6 +158,7 @@ def test_keep8_refusals(B, status, change):
 @pytest.mark.parametrize("status,change", [
     (NULL, dict(pre=None)), (NULL, dict(a=None)), (NULL, dict(q=None)), (NULL, dict(exponents=None)), (SHAPE, dict(act=3)), (SHAPE, dict(act=-1)),
     (SHAPE, dict(f=60)), (SHAPE, dict(format=5)), (UNSUPPORTED, dict(pre=P + 8)), (UNSUPPORTED, dict(a=4 * P + 8)), (UNSUPPORTED, dict(q=2 * P + 8)),
+    (UNSUPPORTED, dict(a=P)), (UNSUPPORTED, dict(q=P + 1008)), (UNSUPPORTED, dict(exponents=4 * P)), (UNSUPPORTED, dict(exponents=2 * P + 511)),
 ])
 def test_act_fwd_keep8_refusals(B, status, change):
     refused(B, status, B.mllm_op_act_fwd_keep8, **{**KEEP, **dict(act=2, pre=P, a=4 * P, f=64), **change})
@@ -166,6 +168,7 @@ def test_act_fwd_keep8_refusals(B, status, change):
     (NULL, dict(da=None)), (NULL, dict(dpre=None)), (NULL, dict(da=None, dpre=None, a=None)), (NULL, dict(q=None)), (SHAPE, dict(act=3)), (SHAPE, dict(f=4)),
     (UNSUPPORTED, dict(da=P + 8)), (UNSUPPORTED, dict(dpre=5 * P + 4)), (UNSUPPORTED, dict(a=4 * P + 2)),
     (UNSUPPORTED, dict(dpre=P)), (UNSUPPORTED, dict(a=P)), (UNSUPPORTED, dict(a=5 * P + 16)), (UNSUPPORTED, dict(act=0, dpre=P + 16)),
+    (UNSUPPORTED, dict(q=P)), (UNSUPPORTED, dict(a=2 * P + 496)), (UNSUPPORTED, dict(exponents=5 * P + 1023)),
 ])
 def test_act_bwd_keep8_refusals(B, status, change):
     refused(B, status, B.mllm_op_act_bwd_keep8, **{**KEEP, **dict(act=2, da=P, dpre=5 * P, a=4 * P, f=64), **change})
@@ -176,10 +179,12 @@ def test_act_bwd_keep8_refusals(B, status, change):
     (SHAPE, dict(k=60)), (SHAPE, dict(n=60)), (SHAPE, dict(n=0)), (SHAPE, dict(t=-1)), (SHAPE, dict(format=2)),
     (SHAPE, dict(t=1 << 20, k=2048)), (SHAPE, dict(t=1 << 20, n=2048)),
     (WORKSPACE, dict(workspace=P + 16)), (WORKSPACE, dict(workspace_bytes=511)), (UNSUPPORTED, dict(q=2 * P + 8)),
+    (UNSUPPORTED, dict(dx=P)), (UNSUPPORTED, dict(dw=4 * P + 16)), (UNSUPPORTED, dict(dx=6 * P)), (UNSUPPORTED, dict(workspace=2 * P)), (UNSUPPORTED, dict(dx=7 * P)),
+    (UNSUPPORTED, dict(dw=2 * P - 4)),
 ])
 def test_linear_bwd_keep8_refusals(B, status, change):
     refused(B, status, B.mllm_op_linear_bwd_keep8,
-            **{**KEEP, **dict(dy=P, w=4 * P, dx=5 * P, dw=6 * P, k=64, n=64, workspace=7 * P, workspace_bytes=1 << 40), **change})
+            **{**KEEP, **dict(dy=P, w=4 * P, dx=5 * P, dw=6 * P, k=64, n=64, workspace=7 * P, workspace_bytes=1 << 16), **change})
 
 
 def test_linear_bwd_keep8_workspace(B):

@@ -233,22 +233,15 @@ def test_special_values(B):
     assert torch.equal(y[same], clean[same])
 
 
-def test_more_rows_than_positions_of_a_grid(B):
-    """Workgroups that go over several stretches of rows: one head of eight pairs, a tenth of the elements checked."""
-    t, axes = 40_000_000, [0] * 4 + [1] * 4
-    x = torch.randn(1 << 20, 16, device="cuda").bfloat16().repeat(t // (1 << 20) + 1, 1)[:t].contiguous()
-    pos = torch.arange(2 * t, device="cuda", dtype=torch.int32).remainder_(613).view(2, t)
-    _, _, table = inputs(1, 16, 1, 613, 8)
-    B.mllm_op_rope_axes(x, x, pos, B.pair_axes(axes), table, 613, t, 1, 16, 16, 16)
-    g = torch.Generator(device="cuda").manual_seed(0)
-    again = torch.randn(1, device="cuda")           # (keeps the allocator's order apart from x)
-    del again
-    rows = torch.randint(0, t, (200_000,), generator=g, device="cuda")
-    rows[:3] = torch.tensor([0, t - 1, 33_554_432], device="cuda")
-    sub = torch.empty(len(rows), 16, dtype=torch.bfloat16, device="cuda")
-    # turned back by the same factors: what went in, to two roundings
-    B.mllm_op_rope_axes(x[rows].contiguous(), sub, pos[:, rows].contiguous(), B.pair_axes(axes), table, 613, len(rows), 1, 16, 16, 16, inverse=1)
-    want = sub.double()
-    forward, size = rotated(sub, pos[:, rows], axes, table, 1, 16, 0)
-    got = x[rows].double()
-    assert bool(((got - forward).abs() <= 3 * 2 ** -8 * size).all()) and torch.isfinite(want).all()
+def test_more_workgroups_than_a_dimension_of_a_grid_takes(B):
+    """A token a workgroup and 2^20 + 5 of them, 9 GB: rows that repeat have the same results, bit for bit."""
+    heads, hd, axes, period = 33, 128, [i % 3 for i in range(64)], 1024
+    t, width = (1 << 20) + 5, heads * hd
+    part, pos, table = inputs(period, width, 3, 613, 64, 1)
+    x = part.repeat(t // period + 1, 1)[:t].contiguous()
+    every = pos.repeat(1, t // period + 1)[:, :t].contiguous()
+    B.mllm_op_rope_axes(x, x, every, B.pair_axes(axes), table, 613, t, heads, hd, width, width)
+    B.mllm_op_rope_axes(part, part, pos, B.pair_axes(axes), table, 613, period, heads, hd, width, width)
+    for r in (0, 100 * period, 508 * period, 1023 * period):        # 508 periods: beyond 2^32 bytes
+        assert torch.equal(x[r:r + period], part)
+    assert torch.equal(x[1 << 20:], part[:5])

@@ -190,6 +190,20 @@ def test_gates(B, gate, t, d):
         check_backward(p, y, *backward(B, p, y, stats))
 
 
+def test_gates_far_out(B):
+    """Where the gate's slope is small it is off by a few roundings of itself, not of 1: 20 FP32 and the exponential's argument of up to 40."""
+    for gate in ("row tanh", "row sigmoid"):
+        p = make(41, 64, "none", "none", False, gate)
+        p["gate"] = torch.linspace(-20, 20, 41, device="cuda")
+        y, n, stats = forward(B, p)
+        check_forward(p, y, n, stats)
+        dx, d_o, grads = backward(B, p, y, stats)
+        v = p["gate"].double()
+        slope = 1 / torch.cosh(v) ** 2 if "tanh" in gate else 1 / (2 + v.exp() + (-v).exp())
+        dots = p["dy"].double() * p["o"].double()
+        assert bool(((grads["gate"].double() - dots.sum(1) * slope).abs() <= 100 * FP32 * dots.abs().sum(1) * slope).all())
+
+
 def test_many_rows(B):
     """Workgroups that go over many rows, and more rows than a dimension of a grid holds workgroups of eight."""
     p = make(20000, 136, "layer", "layer", True, "shared tanh", seed=1)
