@@ -61,6 +61,7 @@ typedef enum {
 enum { MLLM_MASK_BIDIR = 0, MLLM_MASK_CAUSAL = 1 };                       /* per segment */
 enum { MLLM_LAYER_VIT = 0, MLLM_LAYER_DECODER = 1, MLLM_LAYER_PROJECTOR = 2 };
 enum { MLLM_ACT_GELU_ERF = 0, MLLM_ACT_GELU_TANH = 1, MLLM_ACT_SWIGLU = 2 };
+enum { MLLM_LAYER_KEEP_INT8 = 1, MLLM_LAYER_KEEP_E4M3 = 2 };               /* mllm_layer_desc_t.keep8 */
 enum { MLLM_QK_NORM = 1, MLLM_QK_NORM_PER_HEAD = 2 };                     /* flags; PER_HEAD only with QK_NORM */
 
 /*
@@ -94,6 +95,11 @@ enum { MLLM_QK_NORM = 1, MLLM_QK_NORM_PER_HEAD = 2 };                     /* fla
  *              likewise with qkn_k_g; in a DECODER layer this comes before the rotary positions.
  *              With MLLM_QK_NORM_PER_HEAD as well (qk_norm = 3) every head is normalised on its own, as in
  *              mllm_op_qk_norm_rope_fwd, with gains [head_dim] that the heads share.
+ *   keep8 (VIT, DECODER): between forward and backward pass the normalised inputs of the QKV projection and of the MLP (n, n2) and what
+ *              the activation is taken of are kept in 8 bits (the formats of mllm_op_keep8) and the activation itself not at all: about half of the
+ *              layer's part of `saved`.  The forward pass is the same (but for the last bit of an activation that is not formed in the product's
+ *              epilogue); the gradients of W_qkv and of the MLP's matrices, and the
+ *              activation's slopes, are taken at the kept values.
  * Parameter tensors per layer, in order (all bf16, matrices [in, out], vectors [n]):
  *   VIT:       ln1_g, ln1_b, w_qkv [d, 3d], b_qkv, w_o [d, d], b_o, ln2_g, ln2_b,
  *              w_1 [d, f], b_1, w_2 [f, d], b_2
@@ -126,6 +132,8 @@ typedef struct {
                          into one connector row of width merge * d_model (0 or 1: none; not with pool) */
   int32_t qk_norm;    /* VIT / DECODER: MLLM_QK_NORM = RMS-normalise the q row and the k row of every token before
                          attention, with MLLM_QK_NORM_PER_HEAD every head of them (0: none; PROJECTOR: must be 0) */
+  int32_t keep8;      /* VIT / DECODER: MLLM_LAYER_KEEP_* = keep what the backward pass reads of the projections' and the MLP's inputs in 8 bits
+                         (0: as it is; PROJECTOR: must be 0) */
 } mllm_layer_desc_t;
 
 /* Layers in execution order: zero or more VIT, then at most one PROJECTOR, then zero or more

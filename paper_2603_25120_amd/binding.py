@@ -48,7 +48,7 @@ class LayerDescC(C.Structure):
                 ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32), ("d_ff", C.c_int32),
                 ("d_out", C.c_int32), ("act", C.c_int32), ("has_bias", C.c_int32),
                 ("norm_eps", C.c_float), ("rope_base", C.c_float), ("pool", C.c_int32),
-                ("merge", C.c_int32), ("qk_norm", C.c_int32)]
+                ("merge", C.c_int32), ("qk_norm", C.c_int32), ("keep8", C.c_int32)]
 
 
 class StageDescC(C.Structure):
@@ -79,6 +79,7 @@ class BatchC(C.Structure):
 NORM_LAYER, NORM_RMS, NORM_NONE = 0, 1, 2
 GATE_LINEAR, GATE_TANH, GATE_SIGMOID = 0, 1, 2
 KEEP_INT8, KEEP_E4M3 = 0, 1
+LAYER_KEEP_INT8, LAYER_KEEP_E4M3 = 1, 2
 
 
 class ResidualNormC(C.Structure):
@@ -287,7 +288,7 @@ def mllm_stage_create(layers: Sequence) -> int:
     arr = (LayerDescC * len(layers))()
     for i, l in enumerate(layers):
         for f, _ in LayerDescC._fields_:
-            setattr(arr[i], f, getattr(l, f, 0) if f == "qk_norm" else getattr(l, f))
+            setattr(arr[i], f, getattr(l, f, 0) if f in ("qk_norm", "keep8") else getattr(l, f))
     desc = StageDescC(len(layers), arr)
     out = C.c_void_p()
     _check(lib().mllm_stage_create(C.byref(desc), C.byref(out)))

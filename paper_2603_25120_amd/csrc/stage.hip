@@ -84,6 +84,7 @@ mllm_status_t check_layer(const mllm_layer_desc_t& L, int i) {
     if (L.merge < 0 || L.merge > 64) return fail(MLLM_ERR_DESC, "layer %d: the connector's merge width must be in 0..64", i);
     if (L.merge > 1 && L.pool > 1) return fail(MLLM_ERR_DESC, "layer %d: a connector either pools or merges", i);
     if (L.qk_norm != 0) return fail(MLLM_ERR_DESC, "layer %d: a connector has no QK normalisation", i);
+    if (L.keep8 != 0) return fail(MLLM_ERR_DESC, "layer %d: a connector keeps its activations as they are", i);
     if (L.d_ff != 0) {
       if (!m64(L.d_ff)) return fail(MLLM_ERR_DESC, "layer %d: the connector's hidden width must be 0 or a positive multiple of 64", i);
       if (L.act != MLLM_ACT_GELU_ERF && L.act != MLLM_ACT_GELU_TANH) return fail(MLLM_ERR_DESC, "layer %d: an MLP connector's activation must be GELU", i);
@@ -100,6 +101,7 @@ mllm_status_t check_layer(const mllm_layer_desc_t& L, int i) {
   if (!(L.norm_eps > 0.f)) return fail(MLLM_ERR_DESC, "layer %d: norm_eps must be positive", i);
   if (L.qk_norm != 0 && L.qk_norm != MLLM_QK_NORM && L.qk_norm != (MLLM_QK_NORM | MLLM_QK_NORM_PER_HEAD))
     return fail(MLLM_ERR_DESC, "layer %d: qk_norm must be 0, MLLM_QK_NORM or MLLM_QK_NORM | MLLM_QK_NORM_PER_HEAD", i);
+  if (L.keep8 < 0 || L.keep8 > MLLM_LAYER_KEEP_E4M3) return fail(MLLM_ERR_DESC, "layer %d: keep8 must be 0, MLLM_LAYER_KEEP_INT8 or MLLM_LAYER_KEEP_E4M3", i);
   if (L.kind == MLLM_LAYER_VIT) {
     if (L.has_bias != 1) return fail(MLLM_ERR_DESC, "layer %d: ViT layer needs has_bias = 1", i);
     if (L.act != MLLM_ACT_GELU_ERF && L.act != MLLM_ACT_GELU_TANH) return fail(MLLM_ERR_DESC, "layer %d: ViT activation must be GELU", i);
@@ -187,6 +189,8 @@ struct LayerSaved {  // byte offsets into `saved`
   // normalised (and rotated) q and k in the same columns (its v columns are unused).  Per-head norms keep no statistics:
   // a head is read anyway
   size_t qkn, statsq, statsk;
+  // Layers that keep their activations in 8 bits (keep8): n1, n2 and pre then are the kept values, these their exponents; act is not kept
+  size_t n1_e, n2_e, pre_e;
 };
 
 // Attention work lists of one (token space, head counts) combination; layers that agree in these share them.
@@ -218,6 +222,7 @@ struct Plan {
   size_t partial_bytes = 0;
   size_t w_a = 0, w_b = 0, w_c = 0, w_d = 0, w_e = 0, w_delta = 0, w_g0 = 0, w_g1 = 0, w_proj = 0;
   size_t w_qkn = 0;               // QK normalisation: gradient of the normalised q, k  [T, nq]
+  size_t w_keep_n = 0, w_keep_pre = 0, w_keep_act = 0;   // activations kept in 8 bits, in bf16 while they are used  [T, d], [T, f or 2f], [T, f]
   // Rotary-angle tables [longest sample, head_dim] fp32, one per distinct (rope_base, head_dim) of the
   // decoder layers; rope_of[i] = index of layer i's table (-1: the layer has none).
   struct RopeTable { float base; int32_t head_dim; size_t off; };
@@ -311,9 +316,10 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
     }
     const size_t T = L.kind == MLLM_LAYER_VIT ? P.T_img : P.T_seq;
     const size_t d = L.d_model, f = L.d_ff;
+    const size_t fup = L.kind == MLLM_LAYER_VIT ? f : 2 * f, bytes = L.keep8 ? 1 : 2;   // widths are multiples of 64: whole blocks of 32
     S.x = sv.take(T * d * 2);
     S.stats1 = sv.take(T * 2 * 4);
-    S.n1 = sv.take(T * d * 2);
+    S.n1 = sv.take(T * d * bytes);
     S.qkv = sv.take(T * nqkv_of(L) * 2);
     if (L.qk_norm) {
       S.qkn = sv.take(T * nqkv_of(L) * 2);
@@ -326,9 +332,15 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
     S.lse = sv.take(T * L.n_q_heads * 4);
     S.x1 = sv.take(T * d * 2);
     S.stats2 = sv.take(T * 2 * 4);
-    S.n2 = sv.take(T * d * 2);
-    S.pre = sv.take(T * (L.kind == MLLM_LAYER_VIT ? f : 2 * f) * 2);
-    S.act = sv.take(T * f * 2);
+    S.n2 = sv.take(T * d * bytes);
+    S.pre = sv.take(T * fup * bytes);
+    if (L.keep8) {
+      S.n1_e = sv.take(T * d / 32);
+      S.n2_e = sv.take(T * d / 32);
+      S.pre_e = sv.take(T * fup / 32);
+    } else {
+      S.act = sv.take(T * f * 2);
+    }
   }
   P.saved_bytes = std::max<size_t>(sv.off, ALIGN);
 
@@ -371,7 +383,7 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
   }
   M.bytes = ws.off;
 
-  size_t part = 0, part_all = 0, a = 0, bb = 0, c = 0, e = 0, delta = 0, g = 0, proj = 0, qkn = 0;
+  size_t part = 0, part_all = 0, a = 0, bb = 0, c = 0, e = 0, delta = 0, g = 0, proj = 0, qkn = 0, keep_n = 0, keep_pre = 0, keep_act = 0;
   for (const mllm_layer_desc_t& L : st->layers) {
     if (L.kind == MLLM_LAYER_PROJECTOR) {
       proj = (size_t)P.T_con * L.d_out * 2;
@@ -399,6 +411,11 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
     c = std::max(c, T * d * 2);
     e = std::max(e, T * nq * 2);
     if (L.qk_norm) qkn = std::max(qkn, T * nq * 2);
+    if (L.keep8) {
+      keep_n = std::max(keep_n, T * d * 2);
+      keep_pre = std::max(keep_pre, T * (L.kind == MLLM_LAYER_VIT ? f : 2 * f) * 2);
+      keep_act = std::max(keep_act, T * f * 2);
+    }
     delta = std::max(delta, T * L.n_q_heads * 4);
     g = std::max(g, T * d * 2);
   }
@@ -432,6 +449,9 @@ Plan make_plan(const mllm_stage* st, const mllm_batch_t* b, bool scratch = false
   P.w_g0 = ws.take(g);
   P.w_g1 = ws.take(g);
   P.w_proj = ws.take(proj);
+  P.w_keep_n = ws.take(keep_n);
+  P.w_keep_pre = ws.take(keep_pre);
+  P.w_keep_act = ws.take(keep_act);
   P.w_scratch = std::max<size_t>(ws.off, ALIGN);
   if (scratch) {
     size_t split = 0;
@@ -626,13 +646,15 @@ mllm_status_t layer_fwd(const mllm_layer_desc_t& L, const void* const* prm, cons
   const int64_t d = L.d_model, f = L.d_ff, nq = nqkv_of(L);
   const SplitWs split{ws + P.w_scratch, P.scratch_bytes};
   char* x = saved + S.x;
-  char* n1 = saved + S.n1;
+  const bool keep = L.keep8 != 0;                          // in 8 bits: bf16 in the workspace for the products, then kept
+  const int format = L.keep8 - MLLM_LAYER_KEEP_INT8;
+  char* n1 = keep ? ws + P.w_keep_n : saved + S.n1;
   char* qkv = saved + S.qkv;
   char* o = saved + S.o;
   char* x1 = saved + S.x1;
-  char* n2 = saved + S.n2;
-  char* pre = saved + S.pre;
-  char* act = saved + S.act;
+  char* n2 = keep ? ws + P.w_keep_n : saved + S.n2;
+  char* pre = keep ? ws + P.w_keep_pre : saved + S.pre;
+  char* act = keep ? ws + P.w_keep_act : saved + S.act;
   // parameter slots
   const void *g1, *b1n = nullptr, *wqkv, *bqkv = nullptr, *wo, *bo = nullptr, *g2, *b2n = nullptr,
              *wup, *bup = nullptr, *wdn, *bdn = nullptr;
@@ -645,6 +667,7 @@ mllm_status_t layer_fwd(const mllm_layer_desc_t& L, const void* const* prm, cons
 
   // the first layer's input is copied into `saved` by the kernel that reads it anyway
   K_TRY(launch_norm_fwd(vit ? 0 : 1, x_in ? x_in : x, g1, b1n, n1, (float*)(saved + S.stats1), T, d, d, L.norm_eps, s, x_in ? x : nullptr));
+  if (keep) K_TRY(launch_keep8(n1, saved + S.n1, saved + S.n1_e, T, d, d, format, s));
   // Rotary positions ride on the QKV projection's epilogue whenever that product takes the
   // large-tile kernel and nothing sits between the projection and the rotation.
   const bool rope_fused = !vit && !L.qk_norm && (q_cols + k_cols) % 128 == 0 && gemm_rope_fusable(T, nq, d, L.head_dim);
@@ -673,11 +696,16 @@ mllm_status_t layer_fwd(const mllm_layer_desc_t& L, const void* const* prm, cons
   K_TRY(launch_attn_fwd(a, s));
   K_TRY(linear_fwd(o, wo, x1, T, d, d, bo, x, s, split));
   K_TRY(launch_norm_fwd(vit ? 0 : 1, x1, g2, b2n, n2, (float*)(saved + S.stats2), T, d, d, L.norm_eps, s));
+  if (keep) K_TRY(launch_keep8(n2, saved + S.n2, saved + S.n2_e, T, d, d, format, s));
   if (!vit && gemm_swiglu_fusable(T, 2 * f, d)) {
     K_TRY(linear_fwd_swiglu(n2, wup, pre, act, T, d, 2 * f, s));
+    if (keep) K_TRY(launch_keep8(pre, saved + S.pre, saved + S.pre_e, T, 2 * f, 2 * f, format, s));
   } else {
     K_TRY(linear_fwd(n2, wup, pre, T, d, vit ? f : 2 * f, bup, nullptr, s, split));
-    K_TRY(launch_act_fwd(L.act, pre, act, T, f, s));
+    if (keep)
+      K_TRY(launch_act_fwd_keep8(L.act, pre, act, saved + S.pre, saved + S.pre_e, T, f, format, s));
+    else
+      K_TRY(launch_act_fwd(L.act, pre, act, T, f, s));
   }
   K_TRY(linear_fwd(act, wdn, y, T, f, d, bdn, x1, s, split));
   return MLLM_OK;
@@ -693,13 +721,15 @@ mllm_status_t layer_bwd(const mllm_layer_desc_t& L, const void* const* prm, void
   const bool vit = L.kind == MLLM_LAYER_VIT;
   const int64_t d = L.d_model, f = L.d_ff, nq = nqkv_of(L);
   const char* x = saved + S.x;
-  const char* n1 = saved + S.n1;
+  const bool keep = L.keep8 != 0;                          // kept in 8 bits: back to bf16 in the workspace before their use
+  const int format = L.keep8 - MLLM_LAYER_KEEP_INT8;
+  const char* n1 = keep ? ws + P.w_keep_n : saved + S.n1;
   char* qkv = const_cast<char*>(saved + S.qkv);
   const char* o = saved + S.o;
   const char* x1 = saved + S.x1;
-  const char* n2 = saved + S.n2;
-  const char* pre = saved + S.pre;
-  const char* act = saved + S.act;
+  const char* n2 = keep ? ws + P.w_keep_n : saved + S.n2;
+  const char* pre = keep ? ws + P.w_keep_pre : saved + S.pre;
+  const char* act = keep ? ws + P.w_keep_act : saved + S.act;
   const SplitWs split{ws + P.w_scratch, P.scratch_bytes};
   char* wa = ws + P.w_a;      // d act            [T, f]
   char* wb = ws + P.w_b;      // d (gate|up)      [T, 2f]  (decoder)
@@ -715,12 +745,20 @@ mllm_status_t layer_bwd(const mllm_layer_desc_t& L, const void* const* prm, void
   // MLP
   if (vit && !dy_colsum_done) K_TRY(launch_colsum(dy, d, (float*)dprm[ibdn], sums, T, d, s));
   char* dpre = vit ? wa : wb;
-  if (!vit && gemm_swiglu_bwd_fusable(T, f, d)) {
+  const bool fused = !vit && gemm_swiglu_bwd_fusable(T, f, d);
+  if (keep) {
+    K_TRY(launch_act_bwd_keep8(L.act, nullptr, saved + S.pre, saved + S.pre_e, nullptr, ws + P.w_keep_act, T, f, format, s));
+    if (vit || fused) K_TRY(launch_keep8_load(saved + S.pre, saved + S.pre_e, ws + P.w_keep_pre, T, fup, fup, format, s));
+    K_TRY(launch_keep8_load(saved + S.n2, saved + S.n2_e, ws + P.w_keep_n, T, d, d, format, s));
+  }
+  if (fused) {
     K_TRY(linear_bwd(dy, act, prm[iwdn], dpre, dprm[iwdn], T, f, d, accumulate, s, split, pre));
   } else {
     K_TRY(linear_bwd(dy, act, prm[iwdn], wa, dprm[iwdn], T, f, d, accumulate, s, split));
     if (vit)   // the bias gradient (column sums of dpre) comes out of the same pass
       K_TRY(launch_gelu_bwd_colsum(L.act, wa, pre, dpre, (float*)dprm[ibup], sums, T, f, s));
+    else if (keep)
+      K_TRY(launch_act_bwd_keep8(L.act, wa, saved + S.pre, saved + S.pre_e, dpre, nullptr, T, f, format, s));
     else
       K_TRY(launch_act_bwd(L.act, wa, pre, dpre, T, f, s));
   }
@@ -761,6 +799,7 @@ mllm_status_t layer_bwd(const mllm_layer_desc_t& L, const void* const* prm, void
                           T, k_cols, nq, s));
   }
   if (ibqkv >= 0) K_TRY(launch_colsum(we, nq, (float*)dprm[ibqkv], sums, T, nq, s));
+  if (keep) K_TRY(launch_keep8_load(saved + S.n1, saved + S.n1_e, ws + P.w_keep_n, T, d, d, format, s));
   K_TRY(linear_bwd(we, n1, prm[iwqkv], wc, dprm[iwqkv], T, d, nq, accumulate, s, split));
   K_TRY(launch_norm_bwd(vit ? 0 : 1, wc, x, prm[ig1], (const float*)(saved + S.stats1), wd, dx,
                         (float*)dprm[ig1], vit ? (float*)dprm[ib1n] : nullptr, sums, T, d, d, s, dx_colsum));

@@ -192,3 +192,17 @@ def test_linear_bwd_keep8_workspace(B):
     assert size(-1, 64, 64) == 0 and size(4, 0, 64) == 0 and size(4, 64, -8) == 0
     for t, k, n in ((1, 8, 8), (777, 3584, 4608), (8192, 4096, 6144)):
         assert size(t, k, n) >= 2 * t * k and size(t, k, n) - (2 * t * k + 255) // 256 * 256 == B.mllm_linear_bwd_form(t, k, n)[1]
+
+
+def test_layers_that_keep_in_8_bits(B):
+    import dataclasses
+
+    import workloads as W
+    vit, proj, dec = W.tiny_stage_layers()
+    for layers in ([dataclasses.replace(dec, keep8=3)], [dataclasses.replace(dec, keep8=-1)], [dataclasses.replace(vit, keep8=4)],
+                   [vit, dataclasses.replace(proj, keep8=1), dec]):
+        with pytest.raises(B.MllmError) as e:
+            B.mllm_stage_create(layers)
+        assert e.value.status == 2
+    for keep8 in (0, 1, 2):
+        B.mllm_stage_destroy(B.mllm_stage_create([dataclasses.replace(vit, keep8=keep8), proj, dataclasses.replace(dec, keep8=keep8)]))

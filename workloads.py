@@ -71,6 +71,7 @@ class LayerDesc:
     pool: int = 0           # projector: average-pool this many consecutive encoder tokens first (0/1: none)
     merge: int = 0          # projector: concatenate this many consecutive encoder tokens into one row (0/1: none)
     qk_norm: int = 0        # ViT / decoder: RMS-normalise the q rows and the k rows (all heads together; 3: every head) before attention
+    keep8: int = 0          # ViT / decoder: what the backward pass reads of projections' and MLP's inputs is kept in 8 bits (1: int8, 2: e4m3)
 
 
 def vit_layer(d, heads, head_dim, d_ff, eps=1e-5, act=ACT_GELU_ERF, qk_norm=0) -> LayerDesc:
