@@ -673,7 +673,7 @@ mllm_status_t mllm_optimize_parallelism(const mllm_module_profile_t* enc, const 
  * (0 / 1 / 2: the 256x256- and 224x256-tile GEMM kernel in its Y=X.W / dX / dW layouts, 1 also every launch that forms dX and dW together
  * unless both are in 128x128 tiles or quarters of them (then 6): its FLOPs are those of both, its tiles may be 256, 224 or 192 x 256 and
  * 128x128; 3 attention forward,
- * 4 attention backward, 5 the norm / rotary / activation / reduction / copy / embedding / loss kernels, 6 the
+ * 4 attention backward, 5 the norm / rotary / activation / reduction / copy / embedding / loss / residual / 8-bit kernels, 6 the
  * 128x128- and 64x64-tile GEMM kernels in any layout, 7 the 192x256-tile form of the large GEMM kernel in any
  * layout): launches[8], milliseconds[8] and work[8] (algorithmic FLOPs for the GEMM and attention
  * classes, algorithmic bytes for class 5) are host arrays.

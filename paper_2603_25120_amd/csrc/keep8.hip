@@ -100,7 +100,7 @@ __device__ __forceinline__ float normal_below(float v, float& phi) {
   p = fmaf(p, t, 0.0265444126f);
   p = fmaf(p, t, 0.139721021f);
   p = fmaf(p, t, 0.141772136f);
-  p = fmaf(p, t, 0.143713072f);
+  p = fmaf(p, t, 0.14371307f);
   p *= t * e;
   phi = 0.3989422804014327f * e;
   return v < 0.f ? p : 1.f - p;
@@ -122,7 +122,7 @@ __device__ __forceinline__ float activate(float v, float up, float& slope, float
     return v * below;
   }
   // 0.5 v (1 + tanh u) = v logistic(2 u), u = sqrt(2 / pi) (v + 0.044715 v^3)
-  const float v2 = v * v, s = logistic(1.5957691216057308f * v * fmaf(0.044715f, v2, 1.f));
+  const float v2 = fminf(v * v, 1e30f), s = logistic(1.5957691216057308f * v * fmaf(0.044715f, v2, 1.f));
   slope = fmaf(v * s * (1.f - s), 1.5957691216057308f * fmaf(0.134145f, v2, 1.f), s);
   return v * s;
 }

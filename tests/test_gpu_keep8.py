@@ -236,6 +236,20 @@ def test_activations_far_out_and_empty(B, act):
     assert bool(((a.double() - want).abs() <= (HALF + EXP) * want.abs() + TINY)[far].all())
     up = every.double() >= 2.0 ** 40
     assert torch.equal(a[up, 0], every[up])
+    # and backward: the slopes at the kept values, whatever their size (2^128, which the largest are rounded to, aside)
+    value = torch.empty_like(x)
+    B.mllm_op_keep8_load(q, e, value, t, halves * f, B.KEEP_INT8)
+    rows = torch.isfinite(value.float()).all(1)
+    assert (~rows).sum().item() <= 2 * 9
+    da, dpre = torch.ones(t, f, dtype=torch.bfloat16, device="cuda"), torch.empty_like(x)
+    B.mllm_op_act_bwd_keep8(act, da, q, e, dpre, t, f, B.KEEP_INT8)
+    rows &= value.double().abs().amax(1) < (2.0 ** 40 if act == 1 else 2.0 ** 126)      # (the formula in float64 ends at 2^1024: cubes of 2^340)
+    _, slopes, sizes = activation(act, value[rows].double())
+    grad, size = torch.cat(slopes, 1), torch.cat(sizes, 1)
+    assert bool(((dpre[rows].double() - grad).abs() <= HALF * grad.abs() + 4 * EXP * size + TINY).all())
+    far = value.double()[:, 0].abs() >= 2.0 ** 40
+    far &= torch.isfinite(value.double()[:, 0])
+    assert torch.equal(dpre[far, 0].double(), (value[far, 0].double() > 0).double())
     B.mllm_op_act_fwd_keep8(act, None, None, None, None, 0, f, B.KEEP_INT8)
     B.mllm_op_act_bwd_keep8(act, None, None, None, None, 0, f, B.KEEP_INT8)
     x = values(4, halves * 64, 1)
