@@ -1,7 +1,7 @@
 """Build the HIP library in-tree: `python -m paper_2603_25120_amd.build`.
 
 Compiles every source under csrc/ for gfx950 with hipcc and links
-`paper_2603_25120_amd/libmllm_stage.so`.  Objects are cached under `_build/`
+`paper_2603_25120_amd/libmllm_stage.so`, and `_calls.so`, the binding's extension module (host code, g++).  Objects are cached under `_build/`
 (git-ignored); an object is rebuilt when its source or any header is newer.
 """
 from __future__ import annotations
@@ -9,12 +9,14 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(HERE)
 CSRC = os.path.join(HERE, "csrc")
 OUT = os.path.join(HERE, "libmllm_stage.so")
+CALLS = os.path.join(HERE, "_calls.so")
 BUILD = os.path.join(ROOT, "_build")
 
 SOURCES = ["gemm.hip", "gemm_fwd.hip", "gemm_dx.hip", "gemm_dw.hip", "gemm_pair.hip", "gemm_small.hip", "attention.hip", "elementwise.hip", "token.hip", "positions.hip", "residual.hip", "keep8.hip", "stage.hip", "ops_abi.hip", "profile.hip", "scheduler.hip", "planner.hip"]
@@ -49,6 +51,10 @@ def build(force: bool = False, verbose: bool = False) -> str:
         for out in ex.map(_run, jobs):
             if verbose and out.strip():
                 print(out)
+    calls = os.path.join(CSRC, "calls.cpp")
+    if force or not os.path.exists(CALLS) or os.path.getmtime(CALLS) < max(os.path.getmtime(calls), newest_header):
+        _run([os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-fvisibility=hidden", "-I" + sysconfig.get_paths()["include"], calls,
+              "-o", CALLS])
     if jobs or force or not os.path.exists(OUT):
         _run([hipcc, "--offload-arch=gfx950", "-shared", "-fPIC", "-pthread", "-o", OUT] + objs)
     return OUT

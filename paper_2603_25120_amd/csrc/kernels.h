@@ -217,21 +217,20 @@ hipError_t launch_xent(const XentArgs& a, int logits_fp32, hipStream_t s);
 // Rotary positions with several axes (positions.hip).
 struct PositionRun { int32_t row, position, frame_rows, width, step; };   // a stretch of text (frame_rows 0), or a grid whose frames have that many rows
 constexpr int POSITION_RUNS = 192;                                        // in one launch: they travel as the kernel's argument, which holds 4 KB
-struct PositionRuns { PositionRun run[POSITION_RUNS]; };
-// pos [3][stride]: rows row0 .. row0 + rows of a packed sequence, of which the first run begins at row0 and the last one ends there.
-hipError_t launch_grid_positions(const PositionRuns& runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s);
+// pos [3][stride]: rows row0 .. row0 + rows of a packed sequence, of which the first of n runs begins at row0 and the last one ends there.
+hipError_t launch_grid_positions(const PositionRun* runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s);
 constexpr int ROPE_PAIRS = 128, ROPE_AXES = 4;                            // pairs of a head, axes, at most
 struct RopeFrequencies { double frequency[ROPE_PAIRS]; };
 // table [n_pos, 2 n_pairs] fp32: the cosines of row number times frequency, then the sines.
 hipError_t launch_rope_freq_table(float* table, int64_t n_pos, int32_t n_pairs, const RopeFrequencies& f, hipStream_t s);
-// y = x with the pairs (i, i + n_pairs) of each of n_heads heads turned by the table's row pos[axis[i]][row].
+// y = x with the pairs (i, i + n_pairs) of each of n_heads heads turned by the table's row pos[axis of i][row].
 struct RopeAxesArgs {
   const void* x; void* y;
   const int32_t* pos; int64_t pos_stride;
   const float* table; int64_t n_pos;
   int64_t t, x_stride, y_stride;
   int32_t n_heads, head_dim, n_pairs;
-  uint8_t axis[ROPE_PAIRS];
+  uint32_t axes[ROPE_PAIRS / 16];                // two bits a pair
 };
 hipError_t launch_rope_axes(const RopeAxesArgs& a, int inverse, hipStream_t s);
 // The residual stream between two blocks (residual.hip): u = post(o) * scale * gate, y = x + u, n = pre(y).  Kinds: 0 LayerNorm, 1 RMSNorm, 2 none.

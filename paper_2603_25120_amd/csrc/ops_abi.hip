@@ -644,12 +644,12 @@ mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqle
   const int64_t rows = cu_seqlens_host[n_segments];
   if (rows > 0 && !pos) return op_fail(MLLM_ERR_NULL, "pos is NULL");
   if (pos_stride < rows) return op_fail(MLLM_ERR_SHAPE, "pos_stride below the sequence's rows");
-  PositionRuns runs;
+  PositionRun runs[POSITION_RUNS];
   int count = 0;
   return walk_positions(n_segments, cu_seqlens_host, n_grids, grids_host, nullptr, [&](const PositionRun& r, int64_t to) {
-    runs.run[count++] = r;
+    runs[count++] = r;
     if (count == POSITION_RUNS || to == rows) {
-      OP_TRY(launch_grid_positions(runs, count, pos, pos_stride, runs.run[0].row, (int32_t)(to - runs.run[0].row), (hipStream_t)hip_stream));
+      OP_TRY(launch_grid_positions(runs, count, pos, pos_stride, runs[0].row, (int32_t)(to - runs[0].row), (hipStream_t)hip_stream));
       count = 0;
     }
     return MLLM_OK;
@@ -695,7 +695,7 @@ mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int6
   a.n_heads = n_heads; a.head_dim = head_dim; a.n_pairs = n_pairs;
   for (int i = 0; i < n_pairs; i++) {
     if (pair_axis_host[i] >= n_axes) return op_fail(MLLM_ERR_INDEX, "pair %d follows axis %d of %d", i, (int)pair_axis_host[i], n_axes);
-    a.axis[i] = pair_axis_host[i];
+    a.axes[i / 16] |= (uint32_t)pair_axis_host[i] << (2 * (i % 16));
   }
   OP_TRY(launch_rope_axes(a, inverse, (hipStream_t)hip_stream));
   return MLLM_OK;

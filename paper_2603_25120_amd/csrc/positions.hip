@@ -13,9 +13,12 @@ namespace {
 // ---------------------------------------------------------------------------------------------
 // Positions.  A run is a stretch of text or a grid of frames x height x width rows; the host has walked over the samples and knows where
 // every run begins and at which position.  The runs travel as the kernel's argument, so that a call copies nothing and can be captured.  Bound by the
-// launch: 220 rows 1.8 us, 32768 rows of 95 runs 3 to 5.
+// launch: 220 rows 1.8 us, 32768 rows of 95 runs 3 to 5.  Few runs travel by themselves: the host copies the whole argument, 4.5 us a call of 192, 3.6 of 24.
 // ---------------------------------------------------------------------------------------------
-__global__ __launch_bounds__(256) void grid_positions_kernel(PositionRuns runs, int n, int32_t* __restrict__ pos, int64_t stride, int32_t row0, int32_t rows) {
+template <int RUNS>
+struct PositionRuns { PositionRun run[RUNS]; };
+template <int RUNS>
+__global__ __launch_bounds__(256) void grid_positions_kernel(PositionRuns<RUNS> runs, int n, int32_t* __restrict__ pos, int64_t stride, int32_t row0, int32_t rows) {
   __shared__ PositionRun run[256];
   run[threadIdx.x].row = INT32_MAX;
   if ((int)threadIdx.x < n) run[threadIdx.x] = runs.run[threadIdx.x];
@@ -90,7 +93,10 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(RopeAxesArgs a, RopeItem
   fetch(tid);
   for (int i = tid; i < tokens * P; i += 256) {
     const int of = (int)divide((uint32_t)i, it.pairs), pair = i - of * P;
-    const int64_t p = a.pos[a.axis[pair] * a.pos_stride + row0 + of];
+    uint32_t axes = a.axes[0];                // from registers: a load here is one more to wait for before those of position and factors
+#pragma unroll
+    for (int k = 1; k < ROPE_PAIRS / 16; k++) axes = pair >> 4 == k ? a.axes[k] : axes;
+    const int64_t p = a.pos[(axes >> (2 * (pair & 15)) & 3) * a.pos_stride + row0 + of];
     float c = __uint_as_float(0x7fc00000u), s = c;
     if (p >= 0 && p < a.n_pos) {
       c = a.table[p * (2 * P) + pair];
@@ -124,10 +130,23 @@ __global__ __launch_bounds__(256) void rope_axes_kernel(RopeAxesArgs a, RopeItem
 
 }  // namespace
 
-hipError_t launch_grid_positions(const PositionRuns& runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s) {
+namespace {
+template <int RUNS>
+void launch_positions(const PositionRun* runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s) {
+  PositionRuns<RUNS> list;
+  for (int i = 0; i < RUNS; i++) list.run[i] = i < n ? runs[i] : PositionRun{INT32_MAX, 0, 0, 1, 0};
+  hipLaunchKernelGGL(grid_positions_kernel<RUNS>, dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, s, list, n, pos, stride, row0, rows);
+}
+}  // namespace
+
+hipError_t launch_grid_positions(const PositionRun* runs, int n, int32_t* pos, int64_t stride, int32_t row0, int32_t rows, hipStream_t s) {
   if (n <= 0 || rows <= 0) return hipSuccess;
+  if (n > POSITION_RUNS) return hipErrorInvalidValue;
   ProfScope prof(PROF_ELEMENTWISE, 12.0 * rows, s);
-  hipLaunchKernelGGL(grid_positions_kernel, dim3((unsigned)ceil_div(rows, 256)), dim3(256), 0, s, runs, n, pos, stride, row0, rows);
+  if (n <= 24)
+    launch_positions<24>(runs, n, pos, stride, row0, rows, s);
+  else
+    launch_positions<POSITION_RUNS>(runs, n, pos, stride, row0, rows, s);
   return hipGetLastError();
 }
 

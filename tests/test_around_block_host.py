@@ -206,3 +206,56 @@ def test_layers_that_keep_in_8_bits(B):
         assert e.value.status == 2
     for keep8 in (0, 1, 2):
         B.mllm_stage_destroy(B.mllm_stage_create([dataclasses.replace(vit, keep8=keep8), proj, dataclasses.replace(dec, keep8=keep8)]))
+
+
+def test_arguments_of_the_extension_module(B):
+    """What the header's types do not take is refused before the call; None, addresses, tensors and NumPy's numbers are taken."""
+    calls = B._fast()
+    assert set(B.FAST) <= set(B.EXPORTS) and all(callable(getattr(calls, name)) for name in B.FAST)
+
+    class Tensor:
+        def data_ptr(self):
+            return P
+
+    ok = (Tensor(), 2 * P, 3 * P, np.int64(0), np.int32(64), 64, 0, None)         # no rows: nothing is launched
+    assert calls.mllm_op_keep8(*ok) == 0
+    assert calls.mllm_op_keep8(None, None, None, *ok[3:]) == 0
+    assert calls.mllm_op_keep8(None, 2 * P, 3 * P, 4, *ok[4:]) == NULL and "NULL" in B.mllm_last_error()
+    with pytest.raises(TypeError):
+        calls.mllm_op_keep8(*ok[:-1])
+    with pytest.raises(TypeError):
+        calls.mllm_op_keep8(*ok[:4], 64.0, *ok[5:])
+    with pytest.raises(AttributeError):
+        calls.mllm_op_keep8("x", *ok[1:])
+    with pytest.raises(OverflowError):
+        calls.mllm_op_keep8(*ok[:6], 1 << 31, None)
+    with pytest.raises(OverflowError):
+        calls.mllm_op_keep8(*ok[:3], 1 << 63, *ok[4:])
+    with pytest.raises(KeyError):
+        calls.bind("mllm_op_gemm", P)
+    with pytest.raises(ValueError):
+        calls.bind("mllm_op_keep8", 0)
+    assert calls.mllm_op_keep8(*ok) == 0
+
+
+def test_calls_from_several_threads(B):
+    """The status and its message belong to the thread that called."""
+    import threading
+    seen = {}
+
+    def work(i):
+        for _ in range(200):
+            try:
+                if i % 2:
+                    B.mllm_op_keep8(P, 2 * P, 3 * P, 4, 60, 0, stream=1)
+                else:
+                    B.mllm_op_keep8(None, 2 * P, 3 * P, 4, 64, 0, stream=1)
+            except B.MllmError as e:
+                seen.setdefault(i, set()).add((e.status, str(e)))
+
+    threads = [threading.Thread(target=work, args=(i,)) for i in range(6)]
+    for t in threads:
+        t.start()
+    for t in threads:
+        t.join()
+    assert all(len(v) == 1 and next(iter(v))[0] == (SHAPE if i % 2 else NULL) for i, v in seen.items()) and len(seen) == 6

@@ -50,6 +50,8 @@ LAYOUTS = {
     "a sample each": ([0, 9, 9, 18, 30], [(0, 1, 3, 3, 1), (9, 1, 3, 3, 1), (20, 2, 5, 1, 2)]),
     "more runs than a launch takes": (list(range(0, 2001, 8)), [(8 * i + 2, 1, 2, 2, 1) for i in range(250)]),
 }
+LAYOUTS["as many runs as a small launch takes"] = ([0, 24 * 3], [(3 * i, 1, 1, 3, 1) for i in range(24)])
+LAYOUTS["one more than that"] = ([0, 25 * 3], [(3 * i, 1, 1, 3, 1) for i in range(25)])
 LAYOUTS["as many runs as a launch takes"] = ([0, 192 * 3], [(3 * i, 1, 1, 3, 1) for i in range(192)])
 LAYOUTS["one more, and an empty sample behind"] = ([0, 193 * 3, 193 * 3], [(3 * i, 1, 1, 3, 1) for i in range(193)])
 
