@@ -768,6 +768,8 @@ mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const
   if (any_overlap(rx, {rdo}) || bad(rx) || bad(rdo)) return op_fail(MLLM_ERR_UNSUPPORTED, "dx and d_o may each be dn or dy; nothing else may overlap");
   ResidualGrads g = {post ? grads->post_g : nullptr, a.post_kind == MLLM_NORM_LAYER ? grads->post_b : nullptr, a.scale ? grads->scale : nullptr,
                      pre ? grads->pre_g : nullptr, a.pre_kind == MLLM_NORM_LAYER ? grads->pre_b : nullptr, a.gate ? grads->gate : nullptr};
+  if (((uintptr_t)g.post_g | (uintptr_t)g.post_b | (uintptr_t)g.scale | (uintptr_t)g.pre_g | (uintptr_t)g.pre_b) % 16)
+    return op_fail(MLLM_ERR_UNSUPPORTED, "gradients of gains, shifts and scale must start on 16 bytes");
   const Range out[6] = {{g.post_g, 4 * d}, {g.post_b, 4 * d}, {g.scale, 4 * d}, {g.pre_g, 4 * d}, {g.pre_b, 4 * d}, {g.gate, a.gate_per_row ? 4 * t : 4}};
   for (int i = 0; i < 6; i++)
     for (int j = 0; j < i; j++)

@@ -152,6 +152,49 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
   }
 }
 
+// The gradients that follow from the columns' sums A, B, C, D of N columns from col on; a sum that nobody asked for is never used.
+struct FinishArgs {
+  const float* partial; const float* gate_partial;
+  int W, d, sets, accumulate;
+  const bf16_t* post_g; const bf16_t* post_b; const bf16_t* scale;
+  ResidualGrads g;
+};
+// (N columns, a multiple of four, from a multiple of N on.)
+template <int N>
+__device__ __forceinline__ void put_sums(float* out, const float* v, int64_t col, int accumulate) {
+  if (!out) return;
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    float4* o = reinterpret_cast<float4*>(out + col + e);
+    const float4 old = accumulate ? *o : make_float4(0.f, 0.f, 0.f, 0.f);
+    *o = make_float4(v[e] + old.x, v[e + 1] + old.y, v[e + 2] + old.z, v[e + 3] + old.w);
+  }
+}
+template <int N>
+__device__ __forceinline__ void columns_of(const bf16_t* p, int64_t col, float* f, float none) {
+#pragma unroll
+  for (int e = 0; e < N; e += 4) {
+    const uint2 u = p ? *reinterpret_cast<const uint2*>(p + col + e) : make_uint2(0, 0);
+    f[e] = p ? bf16lo(u.x) : none; f[e + 1] = p ? bf16hi(u.x) : none; f[e + 2] = p ? bf16lo(u.y) : none; f[e + 3] = p ? bf16hi(u.y) : none;
+  }
+}
+template <int N>
+__device__ __forceinline__ void put_post(const FinishArgs& a, const float* A, const float* B, int64_t col) {
+  float s[N], g[N], b[N], pg[N], pb[N], sc[N];
+  columns_of<N>(a.scale, col, s, 1.f);
+  columns_of<N>(a.post_g, col, g, 1.f);
+  columns_of<N>(a.post_b, col, b, 0.f);
+#pragma unroll
+  for (int e = 0; e < N; e++) {
+    pg[e] = s[e] * A[e];
+    pb[e] = s[e] * B[e];
+    sc[e] = a.post_b ? fmaf(g[e], A[e], b[e] * B[e]) : g[e] * A[e];
+  }
+  put_sums<N>(a.g.post_g, pg, col, a.accumulate);
+  put_sums<N>(a.g.post_b, pb, col, a.accumulate);
+  put_sums<N>(a.g.scale, sc, col, a.accumulate);
+}
+
 // Backward.  With h the stream without mean, times its factor, z the same of o (o itself without a norm), g the gate:
 //   dY = dy + pre'(dn),  pre'(dn) = factor * (dn pre_g - mean(dn pre_g) - h mean(dn pre_g h));  dx = dY
 //   do = post'(dY g scale post_g), or dY g scale without a norm
@@ -162,7 +205,7 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
 template <int POST, int PRE, bool PAST, int THREADS>
 __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, const bf16_t* dn, const bf16_t* dy, const bf16_t* __restrict__ y,
                                                             const bf16_t* __restrict__ o, const float* __restrict__ stats, bf16_t* dx, bf16_t* d_o,
-                                                            float* __restrict__ gate_rows, float* __restrict__ partial, int waves, int rows, int sets) {
+                                                            float* __restrict__ gate_rows, float* __restrict__ partial, int waves, int rows, FinishArgs finish) {
   __shared__ RowSums sums;
   __shared__ float joined_columns[8 * 512];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), c = (wave % waves) * 64 + lane, of = wave / waves;
@@ -276,12 +319,12 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
     }
     if (there) store16<PAST>(d_o + at, pack8(dz));
   }
-  // Sets of sums in the order of the bits of `sets`; the wavefronts of a column add theirs up through LDS.
+  // Sets of sums in the order of the bits of `sets`; the wavefronts of a column add theirs up through LDS.  One workgroup alone finishes them too.
   const int64_t W = gridDim.x;
   int at_set = 0;
 #pragma unroll
   for (int set = 0; set < 4; set++) {
-    if (!(sets >> set & 1) || (set == 1 && POST != LAYER) || (set == 3 && PRE != LAYER)) continue;   // those are not among the sets
+    if (!(finish.sets >> set & 1) || (set == 1 && POST != LAYER) || (set == 3 && PRE != LAYER)) continue;   // those are not among the sets
     float* v = set == 0 ? A : set == 1 ? Bs : set == 2 ? C : D;
     if (rows > 1) {
       __syncthreads();
@@ -293,12 +336,17 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
 #pragma unroll
           for (int e = 0; e < 8; e++) v[e] += joined_columns[(r * waves + wave) * 512 + e * 64 + lane];
     }
-    if (of == 0 && column) {
+    if (of == 0 && column && W > 1) {
       float4* p = reinterpret_cast<float4*>(partial + ((int64_t)at_set * W + blockIdx.x) * a.d + 8 * c);
       p[0] = make_float4(v[0], v[1], v[2], v[3]);
       p[1] = make_float4(v[4], v[5], v[6], v[7]);
     }
     at_set++;
+  }
+  if (W == 1 && of == 0 && column) {
+    if (finish.sets & 3) put_post<8>(finish, A, Bs, 8 * c);
+    if (finish.sets & 4) put_sums<8>(finish.g.pre_g, C, 8 * c, finish.accumulate);
+    if (finish.sets & 8) put_sums<8>(finish.g.pre_b, D, 8 * c, finish.accumulate);
   }
   if (gate_rows && !a.gate_per_row) {
     __syncthreads();
@@ -307,7 +355,10 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
     if (threadIdx.x == 0) {
       float v = 0.f;
       for (int r = 0; r < rows; r++) v += joined_columns[r];
-      gate_rows[blockIdx.x] = v;
+      if (W > 1)
+        gate_rows[blockIdx.x] = v;
+      else
+        *finish.g.gate = v + (finish.accumulate ? *finish.g.gate : 0.f);
     }
   }
 }
@@ -315,12 +366,6 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
 // What the sums of the workgroups come to: 32 columns a workgroup, a line of 128 bytes, four of them a lane, and every 32nd workgroup's sums in a group of eight
 // lanes, eight of those requested at a time; the groups of a wavefront are added up by exchanges, the wavefronts' sums through LDS.
 // Grid y: A and B with the gradients that follow from both, C, D, the shared gate.
-struct FinishArgs {
-  const float* partial; const float* gate_partial;
-  int W, d, sets, accumulate;
-  const bf16_t* post_g; const bf16_t* post_b; const bf16_t* scale;
-  ResidualGrads g;
-};
 __device__ __forceinline__ float over_groups(float v) {   // lanes 8, 16, ... apart
   v += from_lane<0x128>(v);
   auto w = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
@@ -350,11 +395,7 @@ __global__ __launch_bounds__(256) void residual_finish_kernel(FinishArgs a) {
   const int cg = threadIdx.x & 7, job = blockIdx.y;
   const int64_t col = ((int64_t)blockIdx.x * 8 + cg) * 4;
   const bool valid = col < a.d;
-  auto put = [&](float* out, const float* v) {
-    if (!out || threadIdx.x >= 8 || !valid) return;
-#pragma unroll
-    for (int e = 0; e < 4; e++) out[col + e] = v[e] + (a.accumulate ? out[col + e] : 0.f);
-  };
+  const bool writes = valid && threadIdx.x < 8;
   if (job == 3) {        // the shared gate: one workgroup
     if (!a.gate_partial || blockIdx.x != 0) return;
     float v = 0.f, *red = &part[0][0][0][0];
@@ -371,27 +412,17 @@ __global__ __launch_bounds__(256) void residual_finish_kernel(FinishArgs a) {
     if (!(a.sets >> (job + 1) & 1)) return;
     float v[4];
     finish_sum(sums, a.W, a.d, col, valid, part[0], v);
-    put(job == 1 ? a.g.pre_g : a.g.pre_b, v);
+    if (writes) put_sums<4>(job == 1 ? a.g.pre_g : a.g.pre_b, v, col, a.accumulate);
     return;
   }
   if (!(a.sets & 3)) return;
-  float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f}, pg[4], pb[4], sc[4];
+  float A[4] = {0.f, 0.f, 0.f, 0.f}, B[4] = {0.f, 0.f, 0.f, 0.f};
   if (a.sets & 1) {
     finish_sum(sums, a.W, a.d, col, valid, part[0], A);
     sums += (int64_t)a.W * a.d;
   }
   if (a.sets & 2) finish_sum(sums, a.W, a.d, col, valid, part[1], B);
-  if (!valid) return;
-#pragma unroll
-  for (int e = 0; e < 4; e++) {
-    const float s = a.scale ? bf16lo(a.scale[col + e]) : 1.f, g = a.post_g ? bf16lo(a.post_g[col + e]) : 1.f, b = a.post_b ? bf16lo(a.post_b[col + e]) : 0.f;
-    pg[e] = s * A[e];
-    pb[e] = s * B[e];
-    sc[e] = a.post_b ? fmaf(g, A[e], b * B[e]) : g * A[e];
-  }
-  put(a.g.post_g, pg);
-  put(a.g.post_b, pb);
-  put(a.g.scale, sc);
+  if (writes) put_post<4>(a, A, B, col);
 }
 
 // Wavefronts of a row, rows of a workgroup: eight wavefronts or more.
@@ -399,10 +430,13 @@ inline int row_waves(int64_t d) { return (int)ceil_div(d, 512); }
 inline int rows_of(int waves) { return std::max(1, 8 / waves); }
 // Workgroups, each going over several rows.  Backward one a CU, two where a wavefront has a row of its own (us with 256 and 512: 32768 x 4096 268 and 290,
 // 5125 x 3200 42.6 and 43.4, 2999 x 3584 30.7 and 31.6, 777 x 4096 15.9 and 18, 26496 x 1024 64 and 67.6; 30000 x 256 26.7 and 24); with the next row but one requested too,
-// the same.
+// the same.  One alone where it has no more to do than twice: it finishes the sums itself, without the second launch (8 x 256 5.8 us, 16 x 256 6.7 and with two 8.3, 4096
+// columns of one row 5.4, of two 7.0 and 8.2, of four 9.7 and 8.2).
 inline int64_t bwd_workgroups(int64_t t, int64_t d) {
   const int waves = row_waves(d);
-  return std::max<int64_t>(1, std::min<int64_t>(waves == 1 ? 512 : 256, ceil_div(t, rows_of(waves))));
+  const int64_t blocks = ceil_div(t, rows_of(waves));
+  if (blocks <= 2) return 1;
+  return std::max<int64_t>(1, std::min<int64_t>(waves == 1 ? 512 : 256, blocks));
 }
 // Forward as many of 768 as gives all of them the same number of rows (5125 x 3200 25.1 us, with 256 29.2, a row each 29.1; 2999 x 3584 16.5, 20.3, 20.1; 30000 x 256 14.9,
 // 19.8, 17.1); where the results go past the caches as backward (32768 x 4096 183, with 768 198, a row each 181; 16000 x 8192 176, 178, 233; 65000 x 2048 178, 198,
@@ -439,20 +473,20 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void
   const int sets = (g.post_g || g.scale ? 1 : 0) | (g.post_b || (g.scale && a.post_b) ? 2 : 0) | (g.pre_g ? 4 : 0) | (g.pre_b ? 8 : 0);
   float* gate_partial = g.gate && !a.gate_per_row ? partial + (size_t)__builtin_popcount(sets) * W * a.d : nullptr;
   float* gate_rows = a.gate_per_row ? g.gate : gate_partial;
+  const FinishArgs f = {partial, gate_partial, (int)W, a.d, sets, accumulate, (const bf16_t*)a.post_g, (const bf16_t*)a.post_b, (const bf16_t*)a.scale, g};
   {
     ProfScope prof(PROF_ELEMENTWISE, (4.0 + (dy ? 2 : 0) + (a.pre_kind == NONE ? 0 : 4) + 2) * (double)a.t * a.d, s);
     const bool past = 2 * a.t * a.d >= NT_BYTES;
 #define CALL(POST, PRE)                                                                                                              \
     if (a.post_kind == POST && a.pre_kind == PRE)                                                                                    \
       hipLaunchKernelGGL((64 * waves * rows <= 512 ? (past ? residual_bwd_kernel<POST, PRE, true, 512> : residual_bwd_kernel<POST, PRE, false, 512>) : (past ? residual_bwd_kernel<POST, PRE, true, 1024> : residual_bwd_kernel<POST, PRE, false, 1024>)), dim3((unsigned)W), dim3(64 * waves * rows), 0, s, a, (const bf16_t*)dn, (const bf16_t*)dy, \
-                         (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, sets);
+                         (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, f);
     CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
 #undef CALL
     const hipError_t e = hipGetLastError();
     if (e != hipSuccess) return e;
   }
-  if (!sets && !gate_partial) return hipSuccess;
-  FinishArgs f = {partial, gate_partial, (int)W, a.d, sets, accumulate, (const bf16_t*)a.post_g, (const bf16_t*)a.post_b, (const bf16_t*)a.scale, g};
+  if (W == 1 || (!sets && !gate_partial)) return hipSuccess;
   ProfScope prof(PROF_ELEMENTWISE, 0.0, s);   // the bytes of the sums are counted with their first stage
   hipLaunchKernelGGL(residual_finish_kernel, dim3((unsigned)ceil_div(a.d, 32), 4), dim3(256), 0, s, f);
   return hipGetLastError();

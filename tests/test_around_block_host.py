@@ -123,7 +123,8 @@ GRADS = dict(post_g=10 * P, post_b=11 * P, scale=12 * P, pre_g=13 * P, pre_b=14 
     (UNSUPPORTED, dict(dx=7 * P)), (UNSUPPORTED, dict(dx=P + 16)), (UNSUPPORTED, dict(d_o=2 * P + 496)), (UNSUPPORTED, dict(dx=3 * P)),
     (UNSUPPORTED, dict(d_o=4 * P)), (UNSUPPORTED, dict(dx=P, d_o=P)),
     (UNSUPPORTED, dict(grads=dict(GRADS, pre_g=10 * P))), (UNSUPPORTED, dict(grads=dict(GRADS, gate=14 * P + 252))),
-    (UNSUPPORTED, dict(grads=dict(GRADS, scale=11 * P + 16))),
+    (UNSUPPORTED, dict(grads=dict(GRADS, scale=11 * P + 16))), (UNSUPPORTED, dict(grads=dict(GRADS, pre_b=14 * P + 8))),
+    (UNSUPPORTED, dict(grads=dict(GRADS, post_g=10 * P + 4))),
 ])
 def test_residual_bwd_refusals(B, status, change):
     change = dict(change)
