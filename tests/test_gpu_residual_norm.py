@@ -241,8 +241,9 @@ def test_rows_of_zeros(B):
     check_backward(p, y, *backward(B, p, y, stats))
 
 
-def test_accumulate_and_what_is_not_wanted(B):
-    p = make(77, 640, "layer", "layer", True, "shared tanh")
+@pytest.mark.parametrize("t,d", [(77, 640), (5, 640), (1, 4104), (9, 136)])      # the last three by one workgroup alone
+def test_accumulate_and_what_is_not_wanted(B, t, d):
+    p = make(t, d, "layer", "layer", True, "shared tanh")
     y, _, stats = forward(B, p)
     dx, d_o, once = backward(B, p, y, stats)
     _, _, twice = backward(B, p, y, stats, accumulate=1, start=0.5)
@@ -252,7 +253,7 @@ def test_accumulate_and_what_is_not_wanted(B):
         assert list(alone) == [name] and torch.equal(alone[name], once[name]) and torch.equal(dx1, dx) and torch.equal(d_o1, d_o)
     dx1, d_o1, none = backward(B, p, y, stats, only=())
     assert not none and torch.equal(dx1, dx) and torch.equal(d_o1, d_o)
-    p = make(77, 640, "layer", "layer", True, "row tanh")      # a gate for every row is overwritten, never added to
+    p = make(t, d, "layer", "layer", True, "row tanh")      # a gate for every row is overwritten, never added to
     y, _, stats = forward(B, p)
     _, _, once = backward(B, p, y, stats)
     _, _, twice = backward(B, p, y, stats, accumulate=1, start=0.5)
