@@ -6,7 +6,7 @@
 // e + 127.  A block that holds an infinity or a NaN has the byte 255 and comes back as NaN, all of it.
 // Bound by memory: a thread has eight columns, four neighbouring lanes a block, whose largest magnitude they exchange inside the vector unit.  Measured (us, TB/s of what
 // has to be moved): 8192 x 14336 SwiGLU forward 150, 6.3, backward with the activation again 187, 6.3; GELU 98, 6.0 and 131, 6.3; keeping a matrix 60,
-// 5.9, loading it 57, 6.3; 777 x 4096 SwiGLU 5.8 and 5.9 (as ordinary stores 6.9 and 7.6).
+// 5.9, loading it 57, 6.3; 777 x 4096 SwiGLU 6.1 and 7.6 (results past the caches too 5.8 and 5.9, but the products that follow read them).
 #include <algorithm>
 
 #include "common.h"
