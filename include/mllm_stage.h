@@ -562,9 +562,9 @@ mllm_status_t mllm_op_act_fwd_keep8(int act, const void* pre, void* a, void* q, 
  * the GELU kinds; nothing else may overlap. */
 mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, const void* exponents, void* dpre, void* a, int64_t t,
                                     int64_t f, int format, void* hip_stream);
-/* mllm_op_linear_bwd with x [t, k] kept in 8 bits by mllm_op_keep8.  workspace: mllm_op_linear_bwd_keep8_workspace_bytes, 256-byte aligned; with
- * less a product may be cut into fewer parts, below 2 t k bytes (rounded up to 256) the call is refused.  dx, dw and workspace may not overlap
- * each other or an input. */
+/* mllm_op_linear_bwd with x [t, k] kept in 8 bits by mllm_op_keep8.  workspace: mllm_op_linear_bwd_keep8_workspace_bytes, 256-byte aligned: x, copies of
+ * dy and w where n is no multiple of 64, and parts of the products.  With less a product may be cut into fewer parts or go without the copies (the
+ * same sums in another order); below 2 t k bytes (rounded up to 256) the call is refused.  dx, dw and workspace may not overlap each other or an input. */
 size_t mllm_op_linear_bwd_keep8_workspace_bytes(int64_t t, int64_t k, int64_t n);
 mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void* exponents, const void* w, void* dx, void* dw, int64_t t,
                                        int64_t k, int64_t n, int format, int accumulate, void* workspace, size_t workspace_bytes,

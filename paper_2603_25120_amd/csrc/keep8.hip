@@ -166,6 +166,27 @@ __global__ __launch_bounds__(256) void keep8_load_kernel(const uint8_t* __restri
   store16<PAST>(y + (int64_t)row * y_stride + 8 * c, pack8(f));
 }
 
+// What the gradients of a linear map read where its output width is no multiple of 64: x from its kept values, and dy and w with rows of zeros up to one, in one launch.
+struct Padded { const bf16_t* src; bf16_t* dst; Division per_row; uint32_t count, first; int nvec; };   // first: its first workgroup; nvec: of a row of src
+template <int FORMAT>
+__global__ __launch_bounds__(256) void linear_operands_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ exponent, bf16_t* __restrict__ x, Items it,
+                                                              Padded dy, Padded w) {
+  if (blockIdx.x >= dy.first) {
+    const Padded p = blockIdx.x >= w.first ? w : dy;
+    const uint32_t i = (blockIdx.x - p.first) * 256u + threadIdx.x, row = divide(i, p.per_row), c = i - row * p.per_row.divisor;
+    if (i >= p.count) return;
+    uint4 u = make_uint4(0, 0, 0, 0);
+    if ((int)c < p.nvec) u = *reinterpret_cast<const uint4*>(p.src + ((int64_t)row * p.nvec + c) * 8);
+    store16<false>(p.dst + (int64_t)i * 8, u);
+    return;
+  }
+  const uint32_t i = blockIdx.x * 256u + threadIdx.x, row = divide(i, it.per_row), c = i - row * it.per_row.divisor;
+  if (i >= it.count || (int)c >= it.nvec) return;
+  float f[8];
+  from8<FORMAT>(load8_once(q + ((int64_t)row * it.nvec + c) * 8), exponent[(int64_t)row * (it.per_row.divisor >> 2) + (c >> 2)], f);
+  store16<false>(x + ((int64_t)row * it.nvec + c) * 8, pack8(f));
+}
+
 // a = act(pre), and pre in 8 bits.  SwiGLU: pre = [gate | up], each half a matrix of its own blocks.
 template <int ACT, int FORMAT, bool PAST>
 __global__ __launch_bounds__(256) void act_fwd_keep8_kernel(const bf16_t* __restrict__ pre, bf16_t* __restrict__ a, uint8_t* __restrict__ q,
@@ -273,6 +294,20 @@ hipError_t launch_keep8_load(const void* q, const void* e, void* y, int64_t t, i
     hipLaunchKernelGGL(kernel, grid, dim3(256), 0, s, (const uint8_t*)q + row * width, (const uint8_t*)e + row * ceil_div(width, 32),
                        (bf16_t*)y + row * y_stride, it, y_stride);
   });
+}
+
+hipError_t launch_linear_operands(const void* q, const void* e, void* x, const void* dy, void* dy_padded, const void* w, void* w_padded, int64_t t, int64_t k,
+                                  int64_t n, int64_t n_padded, int format, hipStream_t s) {
+  const int64_t per_row = 4 * ceil_div(k, 32), items = t * per_row, wide = n_padded / 8;
+  if (items >= (int64_t)1 << 31 || t * wide >= (int64_t)1 << 31 || k * wide >= (int64_t)1 << 31) return hipErrorInvalidValue;
+  ProfScope prof(PROF_ELEMENTWISE, 3.03125 * (double)t * (double)k + 4.0 * (double)(t + k) * (double)n, s);
+  const Items it = {division((uint32_t)per_row), (uint32_t)items, (int)(k / 8)};
+  const uint32_t first = (uint32_t)ceil_div(items, 256), second = first + (uint32_t)ceil_div(t * wide, 256);
+  const Padded pd = {(const bf16_t*)dy, (bf16_t*)dy_padded, division((uint32_t)wide), (uint32_t)(t * wide), first, (int)(n / 8)};
+  const Padded pw = {(const bf16_t*)w, (bf16_t*)w_padded, division((uint32_t)wide), (uint32_t)(k * wide), second, (int)(n / 8)};
+  const auto kernel = format == INT8 ? linear_operands_kernel<INT8> : linear_operands_kernel<E4M3>;
+  hipLaunchKernelGGL(kernel, dim3(second + (unsigned)ceil_div(k * wide, 256)), dim3(256), 0, s, (const uint8_t*)q, (const uint8_t*)e, (bf16_t*)x, it, pd, pw);
+  return hipGetLastError();
 }
 
 hipError_t launch_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* e, int64_t t, int64_t f, int format, hipStream_t s) {

@@ -250,6 +250,9 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void
 // Matrices kept in 8 bits (keep8.hip): q [t, width] bytes, e [t, ceil(width / 32)] exponents; format 0 int8, 1 e4m3.
 hipError_t launch_keep8(const void* x, void* q, void* e, int64_t t, int64_t width, int64_t x_stride, int format, hipStream_t s);
 hipError_t launch_keep8_load(const void* q, const void* e, void* y, int64_t t, int64_t width, int64_t y_stride, int format, hipStream_t s);
+// x [t, k] from its kept values, and dy [t, n] and w [k, n] with n_padded columns, zeros behind the n-th.
+hipError_t launch_linear_operands(const void* q, const void* e, void* x, const void* dy, void* dy_padded, const void* w, void* w_padded, int64_t t, int64_t k,
+                                  int64_t n, int64_t n_padded, int format, hipStream_t s);
 hipError_t launch_act_fwd_keep8(int act, const void* pre, void* a, void* q, void* e, int64_t t, int64_t f, int format, hipStream_t s);
 hipError_t launch_act_bwd_keep8(int act, const void* da, const void* q, const void* e, void* dpre, void* a, int64_t t, int64_t f, int format, hipStream_t s);
 hipError_t launch_copy(const void* src, void* dst, size_t bytes, hipStream_t s);

@@ -837,8 +837,20 @@ mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, cons
   return MLLM_OK;
 }
 
+// The gradient of x contracts over n, which the tile kernel takes in multiples of 64 alone; other widths go to the general kernel, or here get copies of dy and w with
+// columns of zeros, in the launch that loads x.  us without and with the copies: 1 x 1000 x 3000 (t x k x n) 34.8 and 15.8, 777 x 256 x 520 17.2 and 10.2, 100 x 200 x 7176
+// 68 and 17, 777 x 7000 x 7000 273 and 211, 2999 x 4104 x 4104 251 and 198, 16000 x 1000 x 3000 207 and 213; many rows of narrow x lose, dy being most of what is read:
+// 16000 x 256 x 136 26.6 and 31.9, 16000 x 72 x 7000 115 and 154 (2999 rows 81 and 38).
+constexpr int64_t PADDED_ROWS = 4096, PADDED_WIDTH = 512;
+static bool takes_copies(int64_t t, int64_t k, int64_t n) { return n % 64 != 0 && (t <= PADDED_ROWS || k >= PADDED_WIDTH); }
+static int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }
+static size_t copies_bytes(int64_t t, int64_t k, int64_t n) { return align_up((size_t)t * padded(n) * 2) + align_up((size_t)k * padded(n) * 2); }
+
 size_t mllm_op_linear_bwd_keep8_workspace_bytes(int64_t t, int64_t k, int64_t n) {
-  return t < 0 || t > MAX_ROWS || k <= 0 || n <= 0 || k > ((int64_t)1 << 30) || n > ((int64_t)1 << 30) ? 0 : align_up((size_t)t * k * 2) + linear_bwd_ws_bytes(t, k, n, false);
+  if (t < 0 || t > MAX_ROWS || k <= 0 || n <= 0 || k > ((int64_t)1 << 30) || n > ((int64_t)1 << 30)) return 0;
+  const int64_t rows = k >= PADDED_WIDTH ? t : std::min(t, PADDED_ROWS);   // so that a buffer for more rows has room for the copies of fewer
+  return align_up((size_t)t * k * 2) + (n % 64 == 0 ? 0 : copies_bytes(rows, k, n)) +
+         std::max(linear_bwd_ws_bytes(t, k, n, false), linear_bwd_ws_bytes(t, k, padded(n), false));
 }
 
 mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void* exponents, const void* w, void* dx, void* dw, int64_t t,
@@ -853,13 +865,29 @@ mllm_status_t mllm_op_linear_bwd_keep8(const void* dy, const void* q, const void
   if (kept && !workspace) return op_fail(MLLM_ERR_NULL, "workspace is NULL");
   if ((uintptr_t)workspace % ALIGN) return op_fail(MLLM_ERR_WORKSPACE, "the workspace must be 256-byte aligned");
   if (workspace_bytes < kept) return op_fail(MLLM_ERR_WORKSPACE, "workspace has %zu bytes, %zu needed", workspace_bytes, kept);
+  if (((uintptr_t)dy | (uintptr_t)w | (uintptr_t)dx | (uintptr_t)dw) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "dy, w, dx and dw must start on 16 bytes");
   CHECK(check_kept(q, exponents, t, k, {{dx, 2 * t * k}, {dw, 4 * k * n}, {workspace, (int64_t)workspace_bytes}}));
   const Range rx = {dx, 2 * t * k}, rw = {dw, 4 * k * n}, rs = {workspace, (int64_t)workspace_bytes}, in[2] = {{dy, 2 * t * n}, {w, 2 * k * n}};
   if (any_overlap(rx, {rw, rs, in[0], in[1]}) || any_overlap(rw, {rs, in[0], in[1]}) || any_overlap(rs, {in[0], in[1]}))
     return op_fail(MLLM_ERR_UNSUPPORTED, "dx, dw and workspace may not overlap each other or an input");
-  OP_TRY(launch_keep8_load(q, exponents, workspace, t, k, k, format, (hipStream_t)hip_stream));
   if (t == 0) return mllm_op_linear_bwd(w, w, w, dw, dw, 0, k, n, accumulate, nullptr, nullptr, 0, hip_stream);   // no rows: none of the rows' matrices is touched
-  return mllm_op_linear_bwd(dy, workspace, w, dx, dw, t, k, n, accumulate, nullptr, (char*)workspace + kept, workspace_bytes - kept, hip_stream);
+  const int64_t wide = padded(n);
+  const size_t copies = copies_bytes(t, k, n);
+  if (!takes_copies(t, k, n) || workspace_bytes < kept + copies || 2 * std::max(t, k) * wide > GEMM_MAX_OPERAND_BYTES) {
+    OP_TRY(launch_keep8_load(q, exponents, workspace, t, k, k, format, (hipStream_t)hip_stream));
+    return mllm_op_linear_bwd(dy, workspace, w, dx, dw, t, k, n, accumulate, nullptr, (char*)workspace + kept, workspace_bytes - kept, hip_stream);
+  }
+  char* dy_padded = (char*)workspace + kept;
+  char* w_padded = dy_padded + align_up((size_t)t * wide * 2);
+  OP_TRY(launch_linear_operands(q, exponents, workspace, dy, dy_padded, w, w_padded, t, k, n, wide, format, (hipStream_t)hip_stream));
+  GemmArgs gx{}, gw{};
+  linear_bwd_args(gx, gw, t, k, n);
+  gx.a = dy_padded; gx.b = w_padded; gx.c = dx; gx.k = gx.lda = gx.ldb = wide;
+  gw.a = workspace; gw.b = dy_padded; gw.c = dw; gw.ldb = wide; gw.accumulate = accumulate;
+  gx.splitk_ws_bytes = gw.splitk_ws_bytes = workspace_bytes - kept - copies;
+  gx.splitk_ws = gw.splitk_ws = gx.splitk_ws_bytes ? (char*)workspace + kept + copies : nullptr;
+  OP_TRY(launch_linear_bwd(gx, gw, (hipStream_t)hip_stream));
+  return MLLM_OK;
 }
 
 }  // extern "C"

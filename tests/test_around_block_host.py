@@ -181,7 +181,7 @@ def test_act_bwd_keep8_refusals(B, status, change):
     (SHAPE, dict(t=1 << 20, k=2048)), (SHAPE, dict(t=1 << 20, n=2048)),
     (WORKSPACE, dict(workspace=P + 16)), (WORKSPACE, dict(workspace_bytes=511)), (UNSUPPORTED, dict(q=2 * P + 8)),
     (UNSUPPORTED, dict(dx=P)), (UNSUPPORTED, dict(dw=4 * P + 16)), (UNSUPPORTED, dict(dx=6 * P)), (UNSUPPORTED, dict(workspace=2 * P)), (UNSUPPORTED, dict(dx=7 * P)),
-    (UNSUPPORTED, dict(dw=2 * P - 4)),
+    (UNSUPPORTED, dict(dw=2 * P - 16)), (UNSUPPORTED, dict(dy=P + 8)), (UNSUPPORTED, dict(w=4 * P + 2)), (UNSUPPORTED, dict(dx=5 * P + 4)), (UNSUPPORTED, dict(dw=6 * P + 8)),
 ])
 def test_linear_bwd_keep8_refusals(B, status, change):
     refused(B, status, B.mllm_op_linear_bwd_keep8,
@@ -191,8 +191,15 @@ def test_linear_bwd_keep8_refusals(B, status, change):
 def test_linear_bwd_keep8_workspace(B):
     size = B.mllm_op_linear_bwd_keep8_workspace_bytes
     assert size(-1, 64, 64) == 0 and size(4, 0, 64) == 0 and size(4, 64, -8) == 0
-    for t, k, n in ((1, 8, 8), (777, 3584, 4608), (8192, 4096, 6144)):
-        assert size(t, k, n) >= 2 * t * k and size(t, k, n) - (2 * t * k + 255) // 256 * 256 == B.mllm_linear_bwd_form(t, k, n)[1]
+    up = lambda v: (v + 255) // 256 * 256
+    for t, k, n in ((1, 64, 64), (777, 3584, 4608), (8192, 4096, 6144)):
+        assert size(t, k, n) - up(2 * t * k) == B.mllm_linear_bwd_form(t, k, n)[1]
+    for t, k, n in ((1, 8, 8), (777, 1000, 3000), (20000, 512, 72)):            # copies of dy and w with whole tiles of columns
+        wide = (n + 63) // 64 * 64
+        assert size(t, k, n) >= up(2 * t * k) + up(2 * t * wide) + up(2 * k * wide)
+    for k, n in ((72, 7000), (256, 136), (600, 1000)):                          # a buffer for more rows has what fewer rows want
+        sizes = [size(t, k, n) - up(2 * t * k) - B.mllm_linear_bwd_form(t, k, (n + 63) // 64 * 64)[1] for t in (1, 1000, 4096, 4097, 30000)]
+        assert sizes == sorted(sizes)
 
 
 def test_layers_that_keep_in_8_bits(B):

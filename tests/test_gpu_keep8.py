@@ -263,7 +263,8 @@ def test_activations_far_out_and_empty(B, act):
 
 
 @pytest.mark.parametrize("name", FORMATS)
-@pytest.mark.parametrize("t,k,n", [(1, 8, 8), (7, 64, 40), (128, 256, 192), (333, 520, 264), (1000, 1024, 512), (2048, 512, 4096)])
+@pytest.mark.parametrize("t,k,n", [(1, 8, 8), (7, 64, 40), (128, 256, 192), (333, 520, 264), (1000, 1024, 512), (2048, 512, 4096),
+                                   (1, 1000, 3000), (100, 72, 1000), (2000, 64, 200), (513, 1000, 72), (4097, 256, 136), (4500, 520, 88), (3, 8, 4088)])
 def test_linear_gradients(B, name, t, k, n):
     g = torch.Generator(device="cuda").manual_seed(t)
     x = values(t, k, t)
@@ -282,18 +283,35 @@ def test_linear_gradients(B, name, t, k, n):
     once = dw.clone()
     B.mllm_op_linear_bwd_keep8(dy, q, e, w, dx, dw, t, k, n, fmt(B, name), ws, accumulate=1)
     assert bool(((dw.double() - 2 * dw_want).abs() <= 4 * (t + 2) * FP32 * dw_size).all())
-    # the same gradients, bit for bit, as from the loaded matrix
+    # the same gradients, bit for bit, as from the loaded matrix, where the products are the same (n a multiple of 64)
     y, dx2, dw2 = torch.empty_like(x), torch.empty_like(x), torch.empty_like(dw)
     B.mllm_op_keep8_load(q, e, y, t, k, fmt(B, name))
     _, want = B.mllm_linear_bwd_form(t, k, n)
     scratch = torch.empty(max(want, 256), dtype=torch.uint8, device="cuda")
     B.mllm_op_linear_bwd(dy, y, w, dx2, dw2, t, k, n, workspace=scratch, scratch_bytes=want)
-    assert torch.equal(dx, dx2) and torch.equal(once, dw2)
+    assert n % 64 or (torch.equal(dx, dx2) and torch.equal(once, dw2))
     least = -(-2 * t * k // 256) * 256          # no more than it cannot do without
     B.mllm_op_linear_bwd_keep8(dy, q, e, w, dx, dw, t, k, n, fmt(B, name), ws, workspace_bytes=least)
     assert bool(((dw.double() - dw_want).abs() <= 2 * t * FP32 * dw_size).all())
     with pytest.raises(B.MllmError):
         B.mllm_op_linear_bwd_keep8(dy, q, e, w, dx, dw, t, k, n, fmt(B, name), ws, workspace_bytes=least - 256)
+
+
+@pytest.mark.parametrize("t,k,n", [(9, 64, 72), (300, 520, 1000), (5000, 64, 72)])
+def test_bad_rows_of_a_linear_map(B, t, k, n):
+    """NaN and infinity in one row of dy: that row of dx, and with the kept values all of dw's columns that it touches; nothing else of dx has other bits."""
+    x, w, dy = values(t, k, 1), (0.05 * torch.randn(k, n, device="cuda")).bfloat16(), torch.randn(t, n, device="cuda").bfloat16()
+    q, e = store(B, x, "int8")
+    ws = torch.full((B.mllm_op_linear_bwd_keep8_workspace_bytes(t, k, n),), 0xFF, dtype=torch.uint8, device="cuda")
+    dx, dw, clean = torch.empty_like(x), torch.empty(k, n, device="cuda"), torch.empty_like(x)
+    B.mllm_op_linear_bwd_keep8(dy, q, e, w, clean, dw, t, k, n, B.KEEP_INT8, ws)
+    before = dw.clone()
+    dy[4, 0], dy[6, n - 1] = float("nan"), float("inf")
+    B.mllm_op_linear_bwd_keep8(dy, q, e, w, dx, dw, t, k, n, B.KEEP_INT8, ws)
+    rows = torch.ones(t, dtype=torch.bool, device="cuda")
+    rows[[4, 6]] = False
+    assert torch.equal(dx[rows], clean[rows]) and torch.isnan(dx[4]).all() and not torch.isfinite(dx[6]).any()
+    assert torch.isnan(dw[:, 0]).all() and torch.equal(dw[:, 1:n - 1], before[:, 1:n - 1])
 
 
 def test_linear_gradients_of_no_rows(B):
