@@ -42,9 +42,9 @@ __device__ __forceinline__ void row_sums(float* v, float (*part)[MAX_WAVES], int
 }
 
 // (factor, mean) of a norm over the row's values.  LayerNorm takes two exchanges, the mean and then the squares about it (every wavefront's mean and squares joined in
-// one exchange: 5125 x 3200 with LayerNorm on both sides 34.9 us, so 33.1).
+// one exchange: 5125 x 3200 with LayerNorm on both sides 34.9 us, so 33.1).  per = 1 / d: a division is some ten instructions (33.1 -> 30.3, backward 48.7 -> 45.1).
 template <int KIND>
-__device__ __forceinline__ void statistics(const float* v, bool there, int d, float eps, float (*part)[3][MAX_WAVES], int waves, int wave, int lane,
+__device__ __forceinline__ void statistics(const float* v, bool there, int d, float per, float eps, float (*part)[3][MAX_WAVES], int waves, int wave, int lane,
                                            float& factor, float& mean) {
   factor = 1.f;
   mean = 0.f;
@@ -55,7 +55,8 @@ __device__ __forceinline__ void statistics(const float* v, bool there, int d, fl
 #pragma unroll
     for (int e = 0; e < 8; e++) sum[0] += v[e];       // zeros behind the row
     row_sums<1>(sum, part[0], waves, wave, lane);
-    mean = sum[0] / (float)d;
+    mean = sum[0] * per;
+    mean = fmaf(fmaf(-mean, (float)d, sum[0]), per, mean);   // the remainder, so that a row of equal values has a mean equal to them
   }
   sum[0] = 0.f;
   if (there)
@@ -65,7 +66,7 @@ __device__ __forceinline__ void statistics(const float* v, bool there, int d, fl
       sum[0] += w * w;
     }
   row_sums<1>(sum, part[1], waves, wave, lane);
-  factor = rsqrtf(sum[0] / (float)d + eps);
+  factor = rsqrtf(sum[0] * per + eps);
 }
 
 __device__ __forceinline__ void load_vector(const bf16_t* p, int c, bool there, float* f) {
@@ -105,6 +106,7 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
     if (PRE != NONE) ng = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_g + 8 * c);
     if (PRE == LAYER) nb = *reinterpret_cast<const uint4*>((const bf16_t*)a.pre_b + 8 * c);
   }
+  const float per = 1.f / (float)a.d;
   int parity = 0;
   for (int64_t base = first; base < a.t; base += step, parity ^= 1) {    // all wavefronts alike: they meet at barriers
     const int64_t row = base + of, at = row * a.d + 8 * c;
@@ -115,7 +117,7 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
     unpack8(qx, w);
     fetch(row + step);
     float factor, mean;
-    statistics<POST>(v, there, a.d, a.post_eps, sums[parity].part[0], waves, wave, lane, factor, mean);
+    statistics<POST>(v, there, a.d, per, a.post_eps, sums[parity].part[0], waves, wave, lane, factor, mean);
     if (POST != NONE) {
       unpack8(pg, g);
       unpack8(pb, b);
@@ -137,7 +139,7 @@ __global__ __launch_bounds__(1024) void residual_fwd_kernel(ResidualArgs a, cons
     if (there) store16<PAST>(y + at, stored);
     if (PRE == NONE) continue;
     unpack8(stored, w);
-    statistics<PRE>(w, there, a.d, a.pre_eps, sums[parity].part[1], waves, wave, lane, factor, mean);
+    statistics<PRE>(w, there, a.d, per, a.pre_eps, sums[parity].part[1], waves, wave, lane, factor, mean);
     unpack8(ng, g);
     unpack8(nb, b);
 #pragma unroll
@@ -201,7 +203,7 @@ __device__ __forceinline__ void put_post(const FinishArgs& a, const float* A, co
 // and, summed over the rows, A = dY g z and B = dY g of every column: post_g's gradient is scale A, post_b's scale B, the scale's
 // post_g A + post_b B; pre_g's and pre_b's are the sums of dn h and dn.  The gate's is the row's sum of dY post(o) scale times its slope.
 // A workgroup goes over rows b, b + B, ...; a lane keeps its columns' sums, which go to `partial`, [set][workgroup][d]; the next row's
-// operands are requested before a row is worked on.  32768 x 4096 with RMSNorm on both sides 265 us (6.1 TB/s), 5125 x 3200 (LayerNorm in front, scale, gates) 38.5 (5.1).
+// operands are requested before a row is worked on.  32768 x 4096 with RMSNorm on both sides 265 us (6.1 TB/s), 5125 x 3200 (LayerNorm in front, scale, gates) 38 (5.2).
 template <int POST, int PRE, bool PAST, int THREADS>
 __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, const bf16_t* dn, const bf16_t* dy, const bf16_t* __restrict__ y,
                                                             const bf16_t* __restrict__ o, const float* __restrict__ stats, bf16_t* dx, bf16_t* d_o,
@@ -225,6 +227,8 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
     }
   }
   float gate_sum = 0.f;
+  const float per = 1.f / (float)a.d;
+  const bool reads_o = POST != NONE || (finish.sets & 3) || gate_rows;   // with neither, its gradient follows from dx alone (40000 x 3200 250 -> 217 us)
   // THREADS: what the registers are dealt by.  Rows of more than 6144 columns with LayerNorm behind the block have none left for the next row's operands (spilled:
   // 28728 x 4544 with LayerNorm on both sides 564 us on the form for 1024 threads, 366 on that for 768).
   constexpr bool AHEAD = !(THREADS == 1024 && POST == LAYER);
@@ -239,7 +243,7 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
       if (PRE != NONE) qn = load16_once(dn + at);
       if (PRE != NONE) qy = load16_once(y + at);
       if (dy) qd = load16_once(dy + at);
-      qo = load16_once(o + at);
+      if (reads_o) qo = load16_once(o + at);
     }
     if (PRE != NONE) f_pre = stats[2 * a.t + row];
     if (PRE == LAYER) m_pre = stats[3 * a.t + row];
@@ -277,8 +281,8 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
       }
       if (AHEAD) fetch(row + step);
       row_sums<PRE == LAYER ? 2 : 1>(s, sums.part[parity][0], waves, wave, lane);
-      s[0] /= (float)a.d;
-      s[1] = PRE == LAYER ? s[1] / (float)a.d : 0.f;
+      s[0] *= per;
+      s[1] = PRE == LAYER ? s[1] * per : 0.f;
 #pragma unroll
       for (int e = 0; e < 8; e++) dY[e] = fmaf(dh[e] - s[1] - h[e] * s[0], r1, dY[e]);
     } else if (AHEAD) {
@@ -315,7 +319,7 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
         }
       }
     }
-    const float t0 = POST != NONE ? s[0] / (float)a.d : 0.f, t1 = POST == LAYER ? s[1] / (float)a.d : 0.f;
+    const float t0 = POST != NONE ? s[0] * per : 0.f, t1 = POST == LAYER ? s[1] * per : 0.f;
 #pragma unroll
     for (int e = 0; e < 8; e++) {
       if (POST != NONE) dz[e] = (dz[e] - t1 - z[e] * t0) * r2;

@@ -241,6 +241,29 @@ def test_rows_of_zeros(B):
     check_backward(p, y, *backward(B, p, y, stats))
 
 
+@pytest.mark.parametrize("d", (8, 1000, 3200, 4104, 8184))
+def test_rows_of_equal_values(B, d):
+    """The mean of equal values is that value (their sum has no more than 24 digits), so that nothing is left of them, whatever eps."""
+    p = make(40, d, "layer", "layer", False, "none")
+    p["x"][:], p["o"][:] = torch.linspace(-300, 500, 40, device="cuda").bfloat16()[:, None], torch.linspace(90, -7, 40, device="cuda").bfloat16()[:, None]
+    p["post_b"][:] = 0
+    y, n, stats = forward(B, p, eps=1e-12)
+    assert torch.equal(y, p["x"]) and torch.equal(n, p["pre_b"].expand(40, -1))
+    assert torch.equal(stats[1], p["o"][:, 0].float()) and torch.equal(stats[3], p["x"][:, 0].float())
+
+
+@pytest.mark.parametrize("scale,gate", [(False, "none"), (True, "row")])
+def test_gradient_of_a_plain_residual(B, scale, gate):
+    """Without a norm behind the block and without the scale's and the gate's gradients its output plays no part."""
+    p = make(300, 1032, "none", "rms", scale, gate)
+    y, _, stats = forward(B, p)
+    want = backward(B, p, y, stats)
+    p["o"] = torch.full_like(p["o"], float("nan"))
+    dx, d_o, grads = backward(B, p, y, stats, only=("pre_g",))
+    assert torch.equal(dx, want[0]) and torch.equal(d_o, want[1]) and torch.equal(grads["pre_g"], want[2]["pre_g"])
+    assert scale or torch.equal(d_o, dx)
+
+
 @pytest.mark.parametrize("t,d", [(77, 640), (5, 640), (1, 4104), (9, 136)])      # the last three by one workgroup alone
 def test_accumulate_and_what_is_not_wanted(B, t, d):
     p = make(t, d, "layer", "layer", True, "shared tanh")
