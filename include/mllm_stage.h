@@ -533,8 +533,9 @@ mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const
                                         int64_t t, int64_t d, void* hip_stream);
 /* Backward, from the gradients dn of n (ignored with pre MLLM_NORM_NONE) and dy of y (bf16 [t, d]; NULL: none, only with a pre norm), and y, o and stats of
  * the forward pass: dx of x, d_o of o (bf16 [t, d]) and the parameters' gradients, of which accumulate != 0 adds to what is there, except
- * the gate's with gate_per_row, which is always overwritten.  dx and d_o may each be dn or dy, and overlap nothing otherwise; the gradients
- * are different buffers.  partial: fp32 scratch of mllm_op_residual_norm_bwd_partial_bytes (the same bytes serve fewer rows of the same d). */
+ * the gate's with gate_per_row, which is always overwritten.  dx and d_o may each be dn or dy; otherwise no output (partial and the parameters' gradients
+ * among them) may overlap an input, a parameter or another output.  partial: fp32 scratch of mllm_op_residual_norm_bwd_partial_bytes (the same bytes
+ * serve fewer rows of the same d). */
 size_t mllm_op_residual_norm_bwd_partial_bytes(int64_t t, int64_t d);
 mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const void* dn, const void* dy, const void* y, const void* o,
                                         const float* stats, void* dx, void* d_o, const mllm_residual_norm_grads_t* grads, int accumulate,

@@ -728,6 +728,11 @@ bool any_overlap(Range a, std::initializer_list<Range> others) {
     if (ranges_overlap(a.p, a.bytes, b.p, b.bytes)) return true;
   return false;
 }
+// The rows of the statistics that the kinds have.
+Range statistics_of(const ResidualArgs& a, const float* stats) {
+  const bool post = a.post_kind != MLLM_NORM_NONE, pre = a.pre_kind != MLLM_NORM_NONE;
+  return {stats && !post ? stats + 2 * a.t : stats, 8 * a.t * (post + pre)};
+}
 }  // namespace
 
 mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const void* x, const void* o, void* y, void* n, float* stats,
@@ -762,18 +767,23 @@ mllm_status_t mllm_op_residual_norm_bwd(const mllm_residual_norm_t* block, const
     return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
   if (((uintptr_t)dn | (uintptr_t)dy | (uintptr_t)y | (uintptr_t)o | (uintptr_t)dx | (uintptr_t)d_o | (uintptr_t)partial) % 16)
     return op_fail(MLLM_ERR_UNSUPPORTED, "dn, dy, y, o, dx, d_o and partial must start on 16 bytes");
-  const int64_t bytes = 2 * t * d;
-  const Range rn = {dn, bytes}, rd = {dy, bytes}, ry = {y, bytes}, ro = {o, bytes}, rx = {dx, bytes}, rdo = {d_o, bytes};
-  const auto bad = [&](Range out) { return (out.p != dn && any_overlap(out, {rn})) || (out.p != dy && any_overlap(out, {rd})) || any_overlap(out, {ry, ro}); };
-  if (any_overlap(rx, {rdo}) || bad(rx) || bad(rdo)) return op_fail(MLLM_ERR_UNSUPPORTED, "dx and d_o may each be dn or dy; nothing else may overlap");
   ResidualGrads g = {post ? grads->post_g : nullptr, a.post_kind == MLLM_NORM_LAYER ? grads->post_b : nullptr, a.scale ? grads->scale : nullptr,
                      pre ? grads->pre_g : nullptr, a.pre_kind == MLLM_NORM_LAYER ? grads->pre_b : nullptr, a.gate ? grads->gate : nullptr};
   if (((uintptr_t)g.post_g | (uintptr_t)g.post_b | (uintptr_t)g.scale | (uintptr_t)g.pre_g | (uintptr_t)g.pre_b) % 16)
     return op_fail(MLLM_ERR_UNSUPPORTED, "gradients of gains, shifts and scale must start on 16 bytes");
-  const Range out[6] = {{g.post_g, 4 * d}, {g.post_b, 4 * d}, {g.scale, 4 * d}, {g.pre_g, 4 * d}, {g.pre_b, 4 * d}, {g.gate, a.gate_per_row ? 4 * t : 4}};
-  for (int i = 0; i < 6; i++)
+  // Workgroups read what others may have written by then: no output shares a byte with an input or another output, but dx and d_o over the gradients that they come from.
+  const int64_t bytes = 2 * t * d, gates = a.gate_per_row ? 4 * t : 4;
+  const Range in[] = {{dn, bytes}, {dy, bytes}, {y, bytes}, {o, bytes}, statistics_of(a, stats), {a.post_g, 2 * d}, {a.post_b, 2 * d}, {a.scale, 2 * d},
+                      {a.pre_g, 2 * d}, {a.pre_b, 2 * d}, {a.gate, gates}};
+  const Range out[] = {{dx, bytes}, {d_o, bytes}, {partial, (int64_t)residual_bwd_partial_floats(t, d) * 4}, {g.post_g, 4 * d}, {g.post_b, 4 * d},
+                       {g.scale, 4 * d}, {g.pre_g, 4 * d}, {g.pre_b, 4 * d}, {g.gate, gates}};
+  for (int i = 0; i < 9; i++) {
+    for (int j = 0; j < 11; j++)
+      if (!(i < 2 && j < 2 && out[i].p == in[j].p) && any_overlap(out[i], {in[j]}))
+        return op_fail(MLLM_ERR_UNSUPPORTED, "dx and d_o may each be dn or dy; no other output may overlap an input");
     for (int j = 0; j < i; j++)
-      if (any_overlap(out[i], {out[j]})) return op_fail(MLLM_ERR_UNSUPPORTED, "two gradients overlap");
+      if (any_overlap(out[i], {out[j]})) return op_fail(MLLM_ERR_UNSUPPORTED, "two outputs overlap");
+  }
   OP_TRY(launch_residual_bwd(a, dn, dy, y, o, stats, dx, d_o, g, accumulate, partial, (hipStream_t)hip_stream));
   return MLLM_OK;
 }
