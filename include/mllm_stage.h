@@ -528,7 +528,7 @@ typedef struct {
   float* gate;
 } mllm_residual_norm_grads_t;
 /* Forward.  n: ignored with pre MLLM_NORM_NONE.  stats fp32 [4, t] for the backward pass: factor and mean of post, factor and mean of pre (rows of a
- * kind that has none are left alone).  y may be x; no other output may overlap an input or another output.  d: a multiple of 8, at most 8192. */
+ * kind that has none are left alone).  y may be x; no other output may overlap an input, a parameter or another output.  d: a multiple of 8, at most 8192. */
 mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const void* x, const void* o, void* y, void* n, float* stats,
                                         int64_t t, int64_t d, void* hip_stream);
 /* Backward, from the gradients dn of n (ignored with pre MLLM_NORM_NONE) and dy of y (bf16 [t, d]; NULL: none, only with a pre norm), and y, o and stats of

@@ -744,9 +744,15 @@ mllm_status_t mllm_op_residual_norm_fwd(const mllm_residual_norm_t* block, const
   if (t > 0 && (!x || !o || !y || (keeps && !stats) || (a.pre_kind != MLLM_NORM_NONE && !n))) return op_fail(MLLM_ERR_NULL, "a tensor pointer is NULL");
   if (((uintptr_t)x | (uintptr_t)o | (uintptr_t)y | (uintptr_t)n) % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "x, o, y and n must start on 16 bytes");
   const int64_t bytes = 2 * t * d;
-  const Range rx = {x, bytes}, ro = {o, bytes}, ry = {y, bytes}, rn = {n, bytes}, rs = {keeps ? stats : nullptr, 16 * t};
-  if ((y != x && any_overlap(ry, {rx})) || any_overlap(ry, {ro, rn, rs}) || any_overlap(rn, {rx, ro, rs}) || any_overlap(rs, {rx, ro}))
-    return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x; nothing else may overlap");
+  const Range in[] = {{x, bytes}, {o, bytes}, {a.post_g, 2 * d}, {a.post_b, 2 * d}, {a.scale, 2 * d}, {a.pre_g, 2 * d}, {a.pre_b, 2 * d}, {a.gate, a.gate_per_row ? 4 * t : 4}};
+  const Range out[] = {{y, bytes}, {n, bytes}, statistics_of(a, stats)};
+  for (int i = 0; i < 3; i++) {
+    for (int j = 0; j < 8; j++)
+      if (!(i == 0 && j == 0 && x == y) && any_overlap(out[i], {in[j]}))
+        return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x; no other output may overlap an input");
+    for (int j = 0; j < i; j++)
+      if (any_overlap(out[i], {out[j]})) return op_fail(MLLM_ERR_UNSUPPORTED, "two outputs overlap");
+  }
   OP_TRY(launch_residual_fwd(a, x, o, y, n, stats, (hipStream_t)hip_stream));
   return MLLM_OK;
 }

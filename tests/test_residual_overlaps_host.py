@@ -77,3 +77,16 @@ def test_gate_of_every_row(B):
         assert overlaps(backward(B, block=each, **{out: PARAMETERS["gate"] + 4 * T - 16}))
     assert overlaps(backward(B, block=each, grads=dict(gate=PARAMETERS["gate"] + 4 * T - 4)))
     assert overlaps(backward(B, block=each, grads=dict(gate=INPUTS["stats"] - 4 * T + 4)))
+
+
+FORWARD = dict(x=P, o=2 * P, y=3 * P, n=4 * P, stats=5 * P)
+
+
+def test_forward_results_that_reach_into_parameters(B):
+    for name, at in PARAMETERS.items():
+        for out, size in (("y", ROWS), ("n", ROWS), ("stats", STATS)):
+            for where in (at, at - size + 16):
+                b = B.ResidualNorm(post_kind=0, pre_kind=0, post_eps=1e-6, pre_eps=1e-6, **PARAMETERS)
+                with pytest.raises(B.MllmError) as e:
+                    B.mllm_op_residual_norm_fwd(b, t=T, d=D, stream=1, **{**FORWARD, out: where})
+                assert e.value.status == UNSUPPORTED and "overlap" in str(e.value), (out, name)
