@@ -494,7 +494,7 @@ mllm_status_t mllm_op_rope_freq_table(float* table, int64_t n_pos, int32_t n_pai
  * [n_axes][pos_stride]; n_axes at most 4), inverse != 0: by the negative angle, which is the gradient; elements from 2 n_pairs on stay as
  * they are.  table: device fp32 [n_pos, 2 n_pairs] from mllm_op_rope_freq_table or mllm_op_rope_table.  A position outside [0, n_pos) reads
  * nothing and makes the row's pairs of that axis NaN.  y receives the same columns, other columns are not touched; y may be x with the same
- * stride and must not overlap it otherwise.  head_dim: a multiple of 8, at most 256; n_pairs: a positive multiple of 8, at most head_dim / 2; n_heads: at
+ * stride and must not overlap it, positions or table otherwise.  head_dim: a multiple of 8, at most 256; n_pairs: a positive multiple of 8, at most head_dim / 2; n_heads: at
  * most 65535. */
 mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int64_t pos_stride, int32_t n_axes,
                                 const uint8_t* pair_axis_host, int32_t n_pairs, const float* table, int64_t n_pos, int64_t t,

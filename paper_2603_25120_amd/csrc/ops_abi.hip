@@ -690,6 +690,10 @@ mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int6
   if ((uintptr_t)table % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "table must start on 16 bytes");
   if (ranges_overlap(x, span_bytes(t, width, x_stride, 2), y, span_bytes(t, width, y_stride, 2)) && (x != y || x_stride != y_stride))
     return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x (same stride) but not overlap it otherwise");
+  const int64_t result = span_bytes(t, width, y_stride, 2);
+  bool over = ranges_overlap(y, result, table, n_pos * n_pairs * 8);
+  for (int axis = 0; axis < n_axes; axis++) over |= pos && ranges_overlap(y, result, pos + axis * pos_stride, 4 * t);
+  if (over) return op_fail(MLLM_ERR_UNSUPPORTED, "y may not overlap positions or table");
   RopeAxesArgs a = {};
   a.x = x; a.y = y; a.pos = pos; a.pos_stride = pos_stride; a.table = table; a.n_pos = n_pos; a.t = t; a.x_stride = x_stride; a.y_stride = y_stride;
   a.n_heads = n_heads; a.head_dim = head_dim; a.n_pairs = n_pairs;
