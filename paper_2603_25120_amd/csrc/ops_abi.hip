@@ -674,6 +674,13 @@ static int64_t span_bytes(int64_t t, int64_t width, int64_t stride, int bytes) {
   return t <= 0 ? 0 : (int64_t)std::min<__int128>(((__int128)(t - 1) * stride + width) * bytes, INT64_MAX / 4);
 }
 
+// Whether two matrices share a byte.  Rows of the same stride may lie in one another's gaps: columns of one buffer beside each other.
+static bool rows_overlap(const void* a, int64_t a_stride, const void* b, int64_t b_stride, int64_t t, int64_t width, int bytes) {
+  if (!ranges_overlap(a, span_bytes(t, width, a_stride, bytes), b, span_bytes(t, width, b_stride, bytes))) return false;
+  const __int128 row = (__int128)a_stride * bytes, apart = (uintptr_t)b > (uintptr_t)a ? (uintptr_t)b - (uintptr_t)a : (uintptr_t)a - (uintptr_t)b;
+  return a_stride != b_stride || apart % row < width * bytes || row - apart % row < width * bytes;
+}
+
 mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int64_t pos_stride, int32_t n_axes,
                                 const uint8_t* pair_axis_host, int32_t n_pairs, const float* table, int64_t n_pos, int64_t t,
                                 int32_t n_heads, int32_t head_dim, int64_t x_stride, int64_t y_stride, int inverse, void* hip_stream) {
@@ -688,7 +695,7 @@ mllm_status_t mllm_op_rope_axes(const void* x, void* y, const int32_t* pos, int6
   CHECK(check_rows("x", x, width, x_stride));
   CHECK(check_rows("y", y, width, y_stride));
   if ((uintptr_t)table % 16) return op_fail(MLLM_ERR_UNSUPPORTED, "table must start on 16 bytes");
-  if (ranges_overlap(x, span_bytes(t, width, x_stride, 2), y, span_bytes(t, width, y_stride, 2)) && (x != y || x_stride != y_stride))
+  if (rows_overlap(x, x_stride, y, y_stride, t, width, 2) && (x != y || x_stride != y_stride))
     return op_fail(MLLM_ERR_UNSUPPORTED, "y may be x (same stride) but not overlap it otherwise");
   const int64_t result = span_bytes(t, width, y_stride, 2);
   bool over = ranges_overlap(y, result, table, n_pos * n_pairs * 8);
