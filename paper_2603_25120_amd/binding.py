@@ -7,13 +7,18 @@ the library's kernels; there is no fallback: a missing library raises.
 from __future__ import annotations
 
 import ctypes as C
+import importlib.machinery
+import importlib.util
+import operator
 import os
+import sysconfig
 from typing import List, Optional, Sequence
 
 import numpy as np
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmllm_stage.so")
+CALLS_PATH = os.path.join(_HERE, "_calls" + sysconfig.get_config_var("EXT_SUFFIX"))
 
 MLLM_OK = 0
 STATUS_NAMES = ["MLLM_OK", "MLLM_ERR_NULL", "MLLM_ERR_DESC", "MLLM_ERR_SHAPE", "MLLM_ERR_CU_SEQLENS",
@@ -33,8 +38,8 @@ EXPORTS = ["mllm_stage_create", "mllm_stage_destroy", "mllm_stage_param_count", 
            "mllm_profile_end", "mllm_schedule_lpt", "mllm_schedule", "mllm_interp", "mllm_item_durations",
            "mllm_find_combs", "mllm_evaluate_parallelism", "mllm_optimize_parallelism"]
 
-# Called through _calls.so, which converts their arguments in a fifth of the time that ctypes takes (220 tokens of 6 heads rotated: 5.2 us a call, of which 2
-# were ctypes and the tensors' addresses).
+# Called through the extension module, which converts their arguments in a fifth of the time that ctypes takes (220 tokens of 6 heads rotated: 5.2 us a call, of
+# which 2 were ctypes and the tensors' addresses).  Where it was not built (no C++ compiler for the host, no Python.h) ctypes takes them.
 FAST = ["mllm_op_grid_positions", "mllm_op_rope_freq_table", "mllm_op_rope_axes", "mllm_op_residual_norm_fwd", "mllm_op_residual_norm_bwd",
         "mllm_op_keep8", "mllm_op_keep8_load", "mllm_op_act_fwd_keep8", "mllm_op_act_bwd_keep8", "mllm_op_linear_bwd_keep8"]
 
@@ -107,7 +112,7 @@ class _BatchAddresses(C.Structure):
 
 
 _lib = None
-_calls = None            # the extension module of FAST (set with the library)
+_calls = None            # the extension module of FAST, or ctypes in its place (set with the library)
 _current_stream = None   # PyTorch's current stream as an address (set with the library)
 
 
@@ -212,11 +217,46 @@ def lib() -> C.CDLL:
     L.mllm_optimize_parallelism.argtypes = [mp, mp, i32, i32, C.c_double, i32, C.c_double, C.c_double, ip, dp, ip]
     for name in EXPORTS:
         getattr(L, name)          # every declared entry point must be exported
-    from . import _calls as calls
+    _calls = _module(L) or _ThroughCtypes(L)
+    _lib = L
+    return L
+
+
+def _module(L: C.CDLL):
+    """The extension module that was built for this interpreter, with the library's entry points, or None."""
+    if not os.path.exists(CALLS_PATH):
+        return None
+    loader = importlib.machinery.ExtensionFileLoader(__package__ + "._calls", CALLS_PATH)
+    calls = importlib.util.module_from_spec(importlib.util.spec_from_file_location(loader.name, CALLS_PATH, loader=loader))
+    loader.exec_module(calls)
     for name in FAST:
         calls.bind(name, C.cast(getattr(L, name), C.c_void_p).value)
-    _lib, _calls = L, calls
-    return L
+    return calls
+
+
+class _ThroughCtypes:
+    """The calls of the extension module by ctypes: the same arguments taken and refused."""
+
+    def __init__(self, L: C.CDLL):
+        for name in FAST:
+            setattr(self, name, self._call(getattr(L, name)))
+
+    @staticmethod
+    def _call(entry):
+        kinds = entry.argtypes
+
+        def whole(kind, v):
+            v = operator.index(v)
+            if kind(v).value != v:
+                raise OverflowError("%d does not fit the argument" % v)
+            return v
+
+        def call(*args):
+            if len(args) != len(kinds):
+                raise TypeError("%d arguments, %d wanted" % (len(args), len(kinds)))
+            return entry(*[_ptr(v) if kind is C.c_void_p else whole(kind, v) for kind, v in zip(kinds, args)])
+
+        return call
 
 
 def _fast():
