@@ -229,8 +229,9 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
   float gate_sum = 0.f;
   const float per = 1.f / (float)a.d;
   const bool reads_o = POST != NONE || (finish.sets & 3) || gate_rows;   // with neither, its gradient follows from dx alone (40000 x 3200 250 -> 217 us)
-  // THREADS: what the registers are dealt by.  Rows of more than 6144 columns with LayerNorm behind the block have none left for the next row's operands (spilled:
-  // 28728 x 4544 with LayerNorm on both sides 564 us on the form for 1024 threads, 366 on that for 768).
+  // THREADS: what the registers are dealt by.  With LayerNorm behind the block and a norm in front of the next one, 1024 threads have none left for the next row's operands (they
+  // spill: us requested ahead and not, LayerNorm on both sides, 16384 x 8192 377 and 323, 2999 x 8192 87 and 74, 16384 x 6152 338 and 271).  Rows of 4104 to 6144 columns have
+  // a form for 768 threads with room for them (28728 x 4544 483 and 358, on 768 284; 2999 x 6144 72, 59, 50).
   constexpr bool AHEAD = !(THREADS == 1024 && POST == LAYER);
   uint4 qn, qd, qy, qo;
   float f_pre, m_pre, f_post, m_post, gate_in;
@@ -371,6 +372,16 @@ __global__ __launch_bounds__(THREADS) void residual_bwd_kernel(ResidualArgs a, c
   }
 }
 
+// The form for a workgroup's threads.  768 is for the kinds that run out of registers on 1024; the others are the same on both (28728 x 4544 RMSNorm on both sides 264 us on either,
+// LayerNorm behind the block alone 227; 2999 x 6144 44.9 and 44.8, 39.3 and 38.6).
+template <int POST, int PRE, bool PAST>
+auto bwd_kernel(int threads) {
+  if (threads <= 512) return residual_bwd_kernel<POST, PRE, PAST, 512>;
+  if constexpr (POST == LAYER && PRE != NONE)
+    if (threads <= 768) return residual_bwd_kernel<POST, PRE, PAST, 768>;
+  return residual_bwd_kernel<POST, PRE, PAST, 1024>;
+}
+
 // What the sums of the workgroups come to: 32 columns a workgroup, a line of 128 bytes, four of them a lane, and every 32nd workgroup's sums in a group of eight
 // lanes, eight of those requested at a time; the groups of a wavefront are added up by exchanges, the wavefronts' sums through LDS.
 // Grid y: A and B with the gradients that follow from both, C, D, the shared gate.
@@ -485,13 +496,11 @@ hipError_t launch_residual_bwd(const ResidualArgs& a, const void* dn, const void
   {
     ProfScope prof(PROF_ELEMENTWISE, (4.0 + (dy ? 2 : 0) + (a.pre_kind == NONE ? 0 : 4) + 2) * (double)a.t * a.d, s);
     const bool past = 2 * a.t * a.d >= NT_BYTES;
+    const int threads = 64 * waves * rows;
 #define CALL(POST, PRE)                                                                                                              \
     if (a.post_kind == POST && a.pre_kind == PRE)                                                                                    \
-      hipLaunchKernelGGL((64 * waves * rows <= 512 ? (past ? residual_bwd_kernel<POST, PRE, true, 512> : residual_bwd_kernel<POST, PRE, false, 512>)  \
-                          : 64 * waves * rows <= 768 ? (past ? residual_bwd_kernel<POST, PRE, true, 768> : residual_bwd_kernel<POST, PRE, false, 768>) \
-                                                     : (past ? residual_bwd_kernel<POST, PRE, true, 1024> : residual_bwd_kernel<POST, PRE, false, 1024>)), \
-                         dim3((unsigned)W), dim3(64 * waves * rows), 0, s, a, (const bf16_t*)dn, (const bf16_t*)dy, \
-                         (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, f);
+      hipLaunchKernelGGL((past ? bwd_kernel<POST, PRE, true>(threads) : bwd_kernel<POST, PRE, false>(threads)), dim3((unsigned)W), dim3(threads), 0, s, a, (const bf16_t*)dn, \
+                         (const bf16_t*)dy, (const bf16_t*)y, (const bf16_t*)o, stats, (bf16_t*)dx, (bf16_t*)d_o, gate_rows, partial, waves, rows, f);
     CALL(LAYER, LAYER) CALL(LAYER, RMS) CALL(LAYER, NONE) CALL(RMS, LAYER) CALL(RMS, RMS) CALL(RMS, NONE) CALL(NONE, LAYER) CALL(NONE, RMS) CALL(NONE, NONE)
 #undef CALL
     const hipError_t e = hipGetLastError();
