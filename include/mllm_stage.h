@@ -479,7 +479,8 @@ mllm_status_t mllm_op_xent(const void* logits, int logits_fp32, const int32_t* t
  * one step.  A grid (an image, or the frames of a clip), grids_host [n_grids][5] = first row, frames, height, width, time step of a frame, covers
  * frames * height * width rows: row (i, j, k) of it has the positions p + i * step, p + j, p + k, and it takes
  * max((frames - 1) * step + 1, height, width) steps.  Grids are in ascending order of their rows and each lies inside one segment
- * (MLLM_ERR_INDEX); sizes are positive, steps not negative (MLLM_ERR_SHAPE).  Any number of grids: up to 192 runs of text or grids go into a launch. */
+ * (MLLM_ERR_INDEX); sizes are positive, steps not negative (MLLM_ERR_SHAPE).  Rows in another order (window by window, as some encoders leave them in front of a
+ * token merge) are no grid in this sense: their positions are the caller's to make.  Any number of grids: up to 192 runs of text or grids go into a launch. */
 mllm_status_t mllm_op_grid_positions(int32_t n_segments, const int32_t* cu_seqlens_host, int32_t n_grids, const int32_t* grids_host,
                                      int32_t* pos, int64_t pos_stride, void* hip_stream);
 /* One more than the largest of these positions: the rows that a table of rotary factors needs (host only, 0 without rows). */

@@ -865,9 +865,10 @@ mllm_status_t mllm_op_act_bwd_keep8(int act, const void* da, const void* q, cons
 }
 
 // The gradient of x contracts over n, which the tile kernel takes in multiples of 64 alone; other widths go to the general kernel, or here get copies of dy and w with
-// columns of zeros, in the launch that loads x.  us without and with the copies: 1 x 1000 x 3000 (t x k x n) 34.8 and 15.8, 777 x 256 x 520 17.2 and 10.2, 100 x 200 x 7176
-// 68 and 17, 777 x 7000 x 7000 273 and 211, 2999 x 4104 x 4104 251 and 198, 16000 x 1000 x 3000 207 and 213; many rows of narrow x lose, dy being most of what is read:
-// 16000 x 256 x 136 26.6 and 31.9, 16000 x 72 x 7000 115 and 154 (2999 rows 81 and 38).
+// columns of zeros, in the launch that loads x.  us without and with the copies: 1 x 1000 x 3000 (t x k x n) 34.8 and 15.8, 777 x 256 x 136 15.5 and 11, 777 x 504 x 3000 45 and 23,
+// 777 x 7000 x 7000 273 and 211, 2999 x 4096 x 4104 250 and 185, 5000 x 1000 x 3000 104 and 82, 8192 x 520 x 3000 93 and 85, 16000 x 2048 x 1000 166 and 161, 30000 x 4096 x 4104 1990 and 1620.  Many rows of
+// narrow x lose, dy being most of what is read: 16000 x 256 x 136 26.6 and 31.9, 16000 x 72 x 7000 115 and 154 (2999 rows 81 and 38).  The border at 512 columns of x is not
+// sharp: 16000 x 520 x 3000 160 and 152, 16000 x 1000 x 3000 188 and 201, 30000 x 520 x 3000 258 and 276, 30000 x 1000 x 3000 364 and 373, 30000 x 600 x 136 63 and 54.
 constexpr int64_t PADDED_ROWS = 4096, PADDED_WIDTH = 512;
 static bool takes_copies(int64_t t, int64_t k, int64_t n) { return n % 64 != 0 && (t <= PADDED_ROWS || k >= PADDED_WIDTH); }
 static int64_t padded(int64_t n) { return (n + 63) / 64 * 64; }

